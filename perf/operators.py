@@ -9,8 +9,9 @@ teacher entries a token.  Kinds:
 
   score    loss and log-sum-exp of every token by its label (evaluation)
   step     the same, then dX and dW of the weighted sum of the losses
-  distill  loss and log-sum-exp by the teacher's top logits, then dX and dW
-  distill_score   the loss and log-sum-exp alone
+  distill  loss, log-sum-exp and the student's logits at the entries by the
+           teacher's top logits, then dX and dW
+  distill_score   the same without the gradients
   lookup   embedding rows of the tokens, scaled
   embgrad  gradient of the embedding from that of its outputs
 
@@ -19,7 +20,8 @@ Formulas, with s_v = x·w_v:
   score    lse = log Σ_v exp(s_v);  loss = lse - s_label  (0 without a label)
   distill  q = softmax(s / t), p = softmax over the teacher's entries of its
            logits / t;  loss = t² Σ_j p_j (log p_j - log q_{i_j});  lse that of
-           s / t; a token without an entry has loss 0
+           s / t, picked_j = s_{i_j} / t (0 where there is no entry); a token
+           without an entry has loss 0
   step     G = weight·(q - onehot(label)), or weight·t·(q - Σ_j p_j onehot(i_j));
            dX = G·W, dW = Gᵀ·X
   lookup   X[n] = scale·E[token_n]  (zeros for a padding token, one below 0)
@@ -183,11 +185,12 @@ def _own(s):
             return dict(loss=loss, lse=lse)
         dX, dW = espace.espace_linear_cross_entropy_backward(s["weight"], X, W, s["labels"], lse)
     else:
-        loss, lse = espace.espace_linear_distillation(X, W, s["index"], s["logits"], temperature=t)
+        loss, lse, picked = espace.espace_linear_distillation(X, W, s["index"], s["logits"], temperature=t)
         if kind == "distill_score":
-            return dict(loss=loss, lse=lse)
-        dX, dW = espace.espace_linear_distillation_backward(s["weight"], X, W, s["index"], s["logits"], lse,
+            return dict(loss=loss, lse=lse, picked=picked)
+        dX, dW = espace.espace_linear_distillation_backward(s["weight"], X, W, s["index"], s["logits"], lse, picked,
                                                             temperature=t)
+        return dict(loss=loss, lse=lse, picked=picked, dX=dX, dW=dW)
     return dict(loss=loss, lse=lse, dX=dX, dW=dW)
 
 
@@ -231,6 +234,8 @@ def run(s):
         at = s["index"].clamp(min=0)
         loss = t * t * (p * torch.where(there, logp - S.gather(1, at) + lse, 0.0)).sum(1, keepdim=True)
     out = dict(loss=loss[:, 0], lse=lse[:, 0])
+    if kind.startswith("distill"):
+        out["picked"] = torch.where(there, S.gather(1, at), 0.0)
     if not kind.endswith("score"):
         G = torch.exp(S - lse)
         G = torch.where(there.any(1, keepdim=True), G, 0.0)
@@ -249,7 +254,7 @@ def work(case):
         return dict(flops=N * K, bytes=2 * e * N * K + 8 * N)
     if kind == "embgrad":
         return dict(flops=N * K, bytes=e * (N * K + V * K) + 8 * N)
-    read = e * (N * K + V * K) + N * (12 * T if T else 8) + 8 * N
+    read = e * (N * K + V * K) + N * (16 * T if T else 8) + 8 * N
     if kind.endswith("score"):
         return dict(flops=2 * N * V * K, bytes=read)
     # the logits' product and the two gradients'
@@ -269,7 +274,7 @@ def exact(case, seed):
         sums = torch.cat([torch.zeros((1, K), dtype=F64, device=DEV), s["dX"][order].cumsum(0)])[ends]
         return (sums[1:] - sums[:-1]) * t
     grads = not kind.endswith("score")
-    loss, lse = [], []
+    loss, lse, picked = [], [], []
     dX, dW = [], torch.zeros((V, K), dtype=F64, device=DEV)
     for n0 in range(0, N, 2048):
         rows = slice(n0, n0 + 2048)
@@ -285,6 +290,9 @@ def exact(case, seed):
             z = torch.full(s["index"][rows].shape, -math.inf, dtype=F64, device=DEV)
             z[n, j] = s["logits"][rows][n, j] / t
             target[n, s["index"][rows][n, j]] = torch.softmax(z, dim=1)[n, j]
+            at = torch.zeros_like(z)
+            at[n, j] = (torch.mm(x, s["W"].t()) / t)[n, s["index"][rows][n, j]]
+            picked.append(at)
         loss.append(t * t * (torch.xlogy(target, target) - target * logq).sum(1))
         if grads:
             G = (torch.exp(logq) * target.sum(1, keepdim=True) - target) * (t * s["weight"][rows][:, None])
@@ -292,6 +300,8 @@ def exact(case, seed):
             dW += torch.mm(G.t(), x)
         del logq, target
     out = dict(loss=torch.cat(loss), lse=torch.cat(lse))
+    if picked:
+        out["picked"] = torch.cat(picked)
     if grads:
         out |= dict(dX=torch.cat(dX), dW=dW)
     return out
