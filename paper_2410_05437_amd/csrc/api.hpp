@@ -1,0 +1,55 @@
+// What the C entry points share (espace_api.hip defines it): statuses, the checks
+// of arguments, and products of two matrices under the library's plans.
+#pragma once
+
+#include "espace.h"
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace espace {
+namespace api {
+
+constexpr int64_t kMaxDim = (int64_t)1 << 30;
+constexpr size_t kWsAlign = 256;
+
+// Sets the thread's last error and returns the status; ok() clears it.
+espace_status fail(espace_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+espace_status ok();
+
+size_t elem_size(espace_dtype dt);
+size_t align_ws(size_t x);
+
+// Compute units of the current device.
+int device_cus();
+
+// An operand's addresses, for the check that no output overlaps it.
+struct Range { const char* name; uintptr_t lo, hi; };
+Range mat_range(const char* name, const void* p, int64_t rows, int64_t ld, espace_dtype dt);
+
+espace_status check_dtype(espace_dtype dt);
+espace_status check_mat(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, espace_dtype dt);
+espace_status check_alias(const Range& out, const Range* ins, int n);
+espace_status check_workspace(void* ws, size_t have, size_t need);
+espace_status check_device();
+
+// C[r][c] = Σ_k A[r][k]·B[c][k], C of type dt, under the library's plan for the sizes;
+// `partial`: run_tn_partial_bytes of scratch.
+size_t run_tn_partial_bytes(int64_t R, int64_t Cc, int64_t D, espace_dtype dt);
+espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R,
+                     int64_t Cc, int64_t D, espace_dtype dt, void* partial, hipStream_t stream);
+
+// The same with C in float32 whatever the operands' type, ldc = splitk_ld(Cc) and C
+// the library's own scratch: columns up to ldc may be written.  Needs no partial sums.
+espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
+                         int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream);
+
+#define ESPACE_TRY(x)                       \
+    do {                                    \
+        espace_status _s = (x);             \
+        if (_s != ESPACE_OK) return _s;     \
+    } while (0)
+
+}  // namespace api
+}  // namespace espace

@@ -17,6 +17,7 @@
 #include <random>
 #include <string>
 
+#include "api.hpp"
 #include "kernels.hpp"
 
 // Scratch of espace_projected_linear_noalloc: Z and the partial sums of one
@@ -28,7 +29,8 @@ static __device__ __align__(256) unsigned char scratch[ESPACE_NOALLOC_SCRATCH_BY
 // the kernels add to it through the address hipGetSymbolAddress gives).
 __device__ unsigned long long g_wait_timeouts;
 
-namespace {
+namespace espace {
+namespace api {
 
 using espace::GemmArgs;
 
@@ -52,9 +54,7 @@ espace_status ok() {
     return ESPACE_OK;
 }
 
-constexpr int64_t kMaxDim = (int64_t)1 << 30;
 constexpr int kDefaultCUs = 256;      // MI355X, for queries made without a device
-constexpr size_t kWsAlign = 256;
 
 size_t elem_size(espace_dtype dt) { return dt == ESPACE_BF16 ? 2 : 4; }
 int64_t ld_align(espace_dtype dt) { return dt == ESPACE_BF16 ? 8 : 4; }
@@ -536,8 +536,6 @@ size_t mx_ws_bytes(int64_t M, int64_t L, int64_t N) {
 
 // ---- validation -------------------------------------------------------------
 
-struct Range { const char* name; uintptr_t lo, hi; };
-
 Range mat_range(const char* name, const void* p, int64_t rows, int64_t ld, espace_dtype dt) {
     const uintptr_t lo = (uintptr_t)p;
     return Range{name, lo, lo + (uintptr_t)(rows * ld) * elem_size(dt)};
@@ -642,12 +640,6 @@ bool autocorr_fits(int64_t K, int64_t N) {
 constexpr int64_t kMaxPcaDim = 32768;
 constexpr int64_t kMaxSymDim = 46340;        // K·round_up(K, 8) < 2^31
 
-#define ESPACE_TRY(x)                       \
-    do {                                    \
-        espace_status _s = (x);             \
-        if (_s != ESPACE_OK) return _s;     \
-    } while (0)
-
 // ---- launch -----------------------------------------------------------------
 
 // One tiled launch of the plan in g.
@@ -671,7 +663,7 @@ hipError_t launch_tiled(const GemmArgs& g, hipStream_t stream) {
 // only for the tiled plans z_pairs admits
 espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
                      int64_t R, int64_t Cc, int64_t D, espace_dtype dt, void* partial,
-                     hipStream_t stream, int a_pairs = 0, int c_pairs = 0, int ranges = kMaxRanges) {
+                     hipStream_t stream, int a_pairs, int c_pairs, int ranges) {
     hipError_t e;
     if (dt == ESPACE_F32) {
         e = espace::launch_gemm_tn_f32((const float*)A, lda, (const float*)B, ldb, (float*)C, ldc,
@@ -737,6 +729,72 @@ espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, voi
             e = espace::launch_stream_tn_bf16(g, stream);
         } else {
             e = launch_tiled(g, stream);
+        }
+    }
+    if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
+    return ESPACE_OK;
+}
+
+espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
+                     int64_t R, int64_t Cc, int64_t D, espace_dtype dt, void* partial, hipStream_t stream) {
+    return run_tn(A, lda, B, ldb, C, ldc, R, Cc, D, dt, partial, stream, 0, 0, kMaxRanges);
+}
+
+size_t run_tn_partial_bytes(int64_t R, int64_t Cc, int64_t D, espace_dtype dt) {
+    return plan_tn(R, Cc, D, dt).partial_bytes;
+}
+
+espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
+                         int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream) {
+    hipError_t e;
+    const int cus = device_cus();
+    if (dt == ESPACE_F32) {
+        e = espace::launch_gemm_tn_f32((const float*)A, lda, (const float*)B, ldb, C, ldc, (int)R, (int)Cc, (int)D,
+                                       cus, stream);
+    } else {
+        GemmArgs g{};
+        g.A = (const uint16_t*)A;
+        g.lda = lda;
+        g.B = (const uint16_t*)B;
+        g.ldb = ldb;
+        g.C = C;
+        g.ldc = ldc;
+        g.R = (int)R;
+        g.Cc = (int)Cc;
+        g.D = (int)D;
+        g.c_f32 = 1;
+        g.splits = 1;
+        g.partial = C;
+        g.cus = cus;
+        const int64_t lim = (int64_t)1 << 31;
+        double us = 0;
+        int config = 0, splits = 1;
+        if (use_gemv((int)R, (int)Cc, (int)D)) {
+            e = espace::launch_gemv_tn_bf16(g, stream);
+        } else {
+            // small tiles up to the token counts of plan_bf16, where they are priced
+            // below a 256 x 256 or 256 x 192 tile per round of workgroups
+            double tiled = 1e300;
+            for (const int bn : {256, 192}) {
+                const int64_t rounds = ceil_div((int64_t)ceil_div(R, 256) * ceil_div(Cc, bn), cus);
+                const double t = 4.75 + kUnitUs * rounds * (256.0 * bn * ceil_div(D, 64) / (bn == 256 ? 1.0 : 0.933) + 101e3);
+                if (t < tiled) {
+                    tiled = t;
+                    g.tile = bn == 256 ? espace::TILE_256x256 : espace::TILE_256x192;
+                }
+            }
+            if (R <= kMidMaxTokens) us = espace::mid_plan((int)R, (int)Cc, (int)D, cus, 1, &config, &splits);
+            if (R <= kMidMaxTokens && us < tiled && espace::mid_supported(lda, ldb)) {
+                g.tile = config;
+                e = espace::launch_mid_tn_bf16(g, stream);
+            } else if (R * lda < lim && Cc * ldb < lim) {
+                int ranges = 1;
+                e = espace::launch_gemm_tn_bf16_v3_ranges(g, false, &ranges, stream);
+            } else {
+                // matrices of 2^31 elements or more: the kernel with 64-bit offsets
+                g.tile = espace::TILE_128x128;
+                e = espace::launch_gemm_tn_bf16(g, stream);
+            }
         }
     }
     if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
@@ -813,7 +871,10 @@ espace_status noalloc_scratch(void** out) {
     return ESPACE_OK;
 }
 
-}  // namespace
+}  // namespace api
+}  // namespace espace
+
+using namespace espace::api;
 
 // The MX-FP8 products after validation.
 // z_pairs: Z's codes in row pairs (ldzq bytes per pair)

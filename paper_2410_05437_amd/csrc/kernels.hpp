@@ -106,6 +106,7 @@ hipError_t launch_gemm_tn_bf16_v3(const GemmArgs& g, hipStream_t stream);
 double mid_plan(int R, int Cc, int D, int cus, int ranges, int* config, int* splits);
 int mid_waves(int config);
 bool mid_supported(int64_t lda, int64_t ldb);
+// c_f32: one range whose fp32 sums are the output (partial = C, ldc = splitk_ld(Cc))
 hipError_t launch_mid_tn_bf16(const GemmArgs& g, hipStream_t stream);
 // Vector-ALU product for 1 <= R <= 2 tokens with whole-row streaming (tile,
 // splits, partial unused); gemv_supported says whether the tokens fit its LDS.

@@ -272,7 +272,8 @@ hipError_t launch_cfg_mid(const GemmArgs& g, bool upper, hipStream_t stream) {
     const int64_t ldp = splitk_ld(g.Cc), stride = (int64_t)g.R * ldp;
     hipLaunchKernelGGL((mid_tn_bf16_kernel<BM, BN, W, ST, SEG>), dim3(tr * tc, S), dim3(W * 64), 0, stream, g.A,
                        g.lda, g.B, g.ldb, (uint16_t*)g.C, g.ldc, g.R, g.Cc, g.D, tc, g.c_pairs,
-                       S > 1 || upper ? g.partial : nullptr, ldp, stride, (steps + S - 1) / S, upper ? 1 : 0);
+                       S > 1 || upper || g.c_f32 ? g.partial : nullptr, ldp, stride, (steps + S - 1) / S,
+                       upper ? 1 : 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || S == 1 || upper) return e;
     return launch_splitk_reduce(g.partial, S, stride, ldp, g.C, g.ldc, g.R, g.Cc, g.c_pairs ? 2 : 1, stream);
@@ -339,7 +340,8 @@ static hipError_t launch_config(const GemmArgs& g, bool upper, hipStream_t strea
 }
 
 hipError_t launch_mid_tn_bf16(const GemmArgs& g, hipStream_t stream) {
-    if (!mid_supported(g.lda, g.ldb) || g.a_pairs || g.c_f32) return hipErrorInvalidValue;
+    if (!mid_supported(g.lda, g.ldb) || g.a_pairs) return hipErrorInvalidValue;
+    if (g.c_f32 && (g.splits > 1 || g.C != g.partial || g.ldc != splitk_ld(g.Cc))) return hipErrorInvalidValue;
     return launch_config(g, false, stream);
 }
 
