@@ -2,7 +2,8 @@
 
 Y = (W·P)·(Pᵀ·X)  (Sakr & Khailany, ESPACE, Section 2.2, Eq. 3), with the
 folded weight W·P computed once and the projection and expansion computed per
-call by hand-written HIP kernels.  Importing the package loads the library;
+call by hand-written HIP kernels; for retraining around such layers, the losses on
+a head's logits and the embedding, with their gradients.  Importing the package loads the library;
 there is no other implementation behind these functions.
 """
 from ._lib import (  # noqa: F401
@@ -44,4 +45,15 @@ from ._lib import (  # noqa: F401
     header_functions,
     lib,
     padded_empty,
+)
+from ._train import (  # noqa: F401
+    MAX_TEACHER_ENTRIES,
+    espace_embedding,
+    espace_embedding_backward,
+    espace_embedding_workspace_bytes,
+    espace_linear_cross_entropy,
+    espace_linear_cross_entropy_backward,
+    espace_linear_distillation,
+    espace_linear_distillation_backward,
+    espace_linear_loss_workspace_bytes,
 )

@@ -15,6 +15,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libespace.so")
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "espace.h")
+TRAIN_HEADER = os.path.join(os.path.dirname(_HERE), "include", "espace_train.h")
 
 F32 = 0
 BF16 = 1
@@ -54,6 +55,18 @@ _SIGS = {
     "espace_project_mxfp8": ([_c_p, _c_i64] * 6 + [_c_i64] * 3 + [_c_p], _c_int),
     "espace_expand_mxfp8": ([_c_p, _c_i64] * 5 + [_c_i64] * 3 + [_c_p], _c_int),
     "espace_projected_linear_mxfp8": ([_c_p, _c_i64] * 7 + [_c_i64] * 4 + [_c_p, _c_sz, _c_p], _c_int),
+    "espace_linear_cross_entropy": ([_c_p, _c_i64] * 2 + [_c_p] * 3 + [_c_i64] * 3 + [_c_int, _c_p, _c_sz, _c_p], _c_int),
+    "espace_linear_cross_entropy_backward": ([_c_p] + [_c_p, _c_i64] * 2 + [_c_p] * 2 + [_c_p, _c_i64] * 2 +
+                                             [_c_i64] * 3 + [_c_int, _c_p, _c_sz, _c_p], _c_int),
+    "espace_linear_distillation": ([_c_p, _c_i64] * 4 + [_c_p] * 2 + [_c_p, _c_i64] + [_c_i64] * 4 +
+                                   [ctypes.c_float, _c_int, _c_p, _c_sz, _c_p], _c_int),
+    "espace_linear_distillation_backward": ([_c_p] + [_c_p, _c_i64] * 4 + [_c_p] + [_c_p, _c_i64] * 3 + [_c_i64] * 4 +
+                                            [ctypes.c_float, _c_int, _c_p, _c_sz, _c_p], _c_int),
+    "espace_linear_loss_workspace_bytes": ([_c_int] + [_c_i64] * 4 + [_c_int], _c_sz),
+    "espace_embedding": ([_c_p] + [_c_p, _c_i64] * 2 + [_c_i64] * 3 + [ctypes.c_float, _c_int, _c_p], _c_int),
+    "espace_embedding_backward": ([_c_p] + [_c_p, _c_i64] * 2 + [_c_i64] * 3 +
+                                  [ctypes.c_float, _c_int, _c_int, _c_p, _c_sz, _c_p], _c_int),
+    "espace_embedding_workspace_bytes": ([_c_i64] * 3, _c_sz),
     "espace_status_string": ([_c_int], ctypes.c_char_p),
     "espace_last_error": ([], ctypes.c_char_p),
     "espace_abi_version": ([], _c_int),
@@ -84,9 +97,9 @@ lib = _load()
 ABI_VERSION = lib.espace_abi_version()
 
 
-def header_functions():
-    """Names of the functions include/espace.h declares."""
-    with open(HEADER) as f:
+def header_functions(header=HEADER):
+    """Names of the functions a header (include/espace.h) declares."""
+    with open(header) as f:
         text = f.read()
     return sorted(set(re.findall(r"^\s*(?:const\s+)?\w+\**\s+\**(espace_\w+)\s*\(", text, re.M)))
 

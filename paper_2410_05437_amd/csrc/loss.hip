@@ -1,0 +1,488 @@
+// Losses on the logits of a linear head, and the gradient of those logits, in pieces
+// of the vocabulary.
+//
+// With s_v = x·w_v / t, a token's log-sum-exp over the vocabulary is that of its
+// pieces: each gives its largest s and Σ exp(s - it), and lse = m + log Σ_pieces
+// l·exp(m_piece - m) is exact however the vocabulary is cut.  Pieces are joined in
+// their order, so that the same call gives the same bits.  The gradient of the logits
+// needs lse alone, G = coef·(exp(s - lse) - p), so a piece of it is made from a piece
+// of the logits, used in both gradients' products, and dropped.
+//
+// Everything is float32 up to G, which is rounded to bfloat16 for the matrix cores
+// once, relative to the largest coefficient c (most training steps weigh all tokens
+// alike: r = coef / c is then 1, and an entry -r of a label with a small probability
+// is exact); c multiplies the float32 sums.
+#include <math.h>
+
+#include "common.hpp"
+#include "kernels.hpp"
+#include "train.hpp"
+
+namespace espace {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float exp_f(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float nan_f() { return __builtin_nanf(""); }
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// Σ exp(s - m) of a set, given that of its parts: l·exp(m_part - m), 0 for a part whose
+// logits are all -infinity
+__device__ __forceinline__ float rescale(float l, float from, float to) {
+    return from == -INFINITY ? 0.f : l * exp_f(from - to);
+}
+
+// ---- targets -------------------------------------------------------------------
+
+// One wave per token, entry 64 u + lane in register u.
+template <int U>
+__global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict__ index, int64_t ldi,
+                                                      const float* __restrict__ logits, int64_t ldl, int N, int T,
+                                                      int V, float inv_t, int merge, int* __restrict__ col,
+                                                      float* __restrict__ p_out, float* __restrict__ logp_out,
+                                                      float* __restrict__ mass) {
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (n >= N) return;
+    int c[U];
+    float z[U];
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int j = 64 * u + lane;
+        c[u] = -1;
+        z[u] = -INFINITY;
+        if (j < T) {
+            const int64_t i = index[(int64_t)n * ldi + j];
+            if (i >= 0) {
+                z[u] = i < V ? logits[(int64_t)n * ldl + j] * inv_t : nan_f();
+                c[u] = i < V ? (int)i : V - 1;
+            }
+        }
+        m = fmaxf(m, z[u]);
+    }
+    m = wave_max(m);
+    float l = 0.f, p[U], lp[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        p[u] = z[u] == -INFINITY ? 0.f : exp_f(z[u] - m);
+        l += p[u];
+    }
+    l = wave_sum(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float lg = logf(l);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        p[u] *= inv;
+        lp[u] = z[u] == -INFINITY ? 0.f : (z[u] - m) - lg;
+    }
+    if (merge) {
+        // every entry against all, in their order: the sum goes to the first place
+        float sum[U];
+        bool again[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            sum[u] = 0.f;
+            again[u] = false;
+        }
+#pragma unroll
+        for (int v = 0; v < U; ++v)
+            for (int k = 0; k < 64 && 64 * v + k < T; ++k) {
+                const int ck = __builtin_amdgcn_readlane(c[v], k);
+                const float pk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p[v]), k));
+                const int j = 64 * v + k;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c[u] == ck) {
+                        sum[u] += pk;
+                        again[u] |= j < 64 * u + lane;
+                    }
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            p[u] = sum[u];
+            if (again[u]) c[u] = -1;
+        }
+        // l is 0 without a target, NaN where an entry is
+        if (lane == 0) mass[n] = l == 0.f ? 0.f : 1.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int j = 64 * u + lane;
+        if (j < T) {
+            col[(int64_t)n * T + j] = c[u];
+            p_out[(int64_t)n * T + j] = p[u];
+            if (logp_out) logp_out[(int64_t)n * T + j] = lp[u];
+        }
+    }
+}
+
+// ---- forward -------------------------------------------------------------------
+
+// STAT_COLS columns of one token: 256 threads of 4 x 4 columns each, kept in
+// registers between the maximum and the sum.
+__global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S, int64_t lds, int c0, int cols,
+                                                    float inv_t, LossTargets t, float2* __restrict__ part, int ldpart,
+                                                    int part0, float* __restrict__ picked, int64_t ldpk) {
+    __shared__ float red[8];
+    const int n = blockIdx.y;
+    const int b0 = blockIdx.x * STAT_COLS;
+    const int left = cols - b0 < STAT_COLS ? cols - b0 : STAT_COLS;
+    const float* row = S + (int64_t)n * lds + b0;
+    float v[4][4];
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = i * 1024 + threadIdx.x * 4;
+        // rows are padded to a multiple of 8 columns
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+        if (c < left) x = *reinterpret_cast<const f32x4_t*>(row + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[i][e] = c + e < left ? x[e] * inv_t : -INFINITY;
+            m = fmaxf(m, v[i][e]);
+        }
+    }
+    m = wave_max(m);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0) red[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float l = 0.f;
+    // all -infinity: the sum stays 0, and NaN (which a maximum passes over) stays NaN
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l += exp_f(v[i][e] - base);
+    l = wave_sum(l);
+    if (lane == 0) red[4 + wave] = l;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        l = (red[4] + red[5]) + (red[6] + red[7]);
+        part[(int64_t)n * ldpart + part0 + blockIdx.x] = make_float2(l == 0.f ? -INFINITY : base, l);
+    }
+    for (int j = threadIdx.x; j < t.T; j += 256) {
+        const int64_t c = (t.labels ? t.labels[n] : (int64_t)t.col[(int64_t)n * t.T + j]) - c0 - b0;
+        if (c >= 0 && c < left) picked[(int64_t)n * ldpk + j] = row[c] * inv_t;
+    }
+}
+
+// One wave per token.
+__global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ part, int ldpart, int nparts, int N,
+                                                     int V, float tt, LossTargets t, float* __restrict__ picked,
+                                                     int64_t ldpk, float* __restrict__ loss, float* __restrict__ lse) {
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (n >= N) return;
+    float m = -INFINITY, l = 0.f;
+    for (int i = lane; i < nparts; i += 64) {
+        const float2 q = part[(int64_t)n * ldpart + i];
+        const float to = fmaxf(m, q.x);
+        l = rescale(l, m, to) + rescale(q.y, q.x, to);
+        m = to;
+    }
+    const float top = wave_max(m);
+    l = wave_sum(rescale(l, m, top));
+    const float ls = top + logf(l);
+    float v = 0.f;
+    if (t.labels) {
+        const int64_t c = t.labels[n];
+        if (c >= V) v = nan_f();
+        else if (c >= 0) v = ls - picked[(int64_t)n * ldpk];
+    } else {
+        for (int j = lane; j < t.T; j += 64) {
+            const int64_t at = (int64_t)n * t.T + j;
+            if (t.col[at] < 0) {
+                picked[(int64_t)n * ldpk + j] = 0.f;
+            } else if (t.p[at] != 0.f) {
+                v += t.p[at] * ((t.logp[at] + ls) - picked[(int64_t)n * ldpk + j]);
+            }
+        }
+        v = wave_sum(v) * tt;
+    }
+    if (lane == 0) {
+        loss[n] = v;
+        lse[n] = ls;
+    }
+}
+
+// ---- backward ------------------------------------------------------------------
+
+// One workgroup: two passes over the tokens.
+__global__ __launch_bounds__(1024) void coef_kernel(const float* __restrict__ dloss,
+                                                    const int64_t* __restrict__ labels,
+                                                    const float* __restrict__ mass, float t, int N, int V,
+                                                    float* __restrict__ r, float* __restrict__ scale) {
+    __shared__ float red[16];
+    auto coef = [&](int n) {
+        if (labels) return labels[n] < 0 ? 0.f : (labels[n] >= V ? nan_f() : dloss[n]);
+        return mass[n] == 0.f ? 0.f : dloss[n] * t;
+    };
+    float m = 0.f;
+    for (int n = threadIdx.x; n < N; n += 1024) {
+        const float a = fabsf(coef(n));
+        if (a < INFINITY) m = fmaxf(m, a);
+    }
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = red[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, red[i]);
+    if (m < 1.17549435e-38f) m = 1.f;             // all 0, or too small to divide by
+    for (int n = threadIdx.x; n < N; n += 1024) r[n] = coef(n) / m;
+    if (threadIdx.x == 0) scale[0] = m;
+}
+
+__device__ __forceinline__ uint16_t to_elem(float v, uint16_t) { return (uint16_t)bf16_rne(v); }
+__device__ __forceinline__ float to_elem(float v, float) { return v; }
+
+// 64 x 64 of G, its transpose through LDS.
+template <typename E>
+__global__ __launch_bounds__(256) void grad_kernel(const float* __restrict__ S, int64_t lds, int N, int c0, int cols,
+                                                   float inv_t, const float* __restrict__ lse,
+                                                   const float* __restrict__ r, const int64_t* __restrict__ labels,
+                                                   E* __restrict__ G, int64_t ldg, E* __restrict__ GT, int64_t ldgt) {
+    __shared__ E tile[64][64 + 4 / sizeof(E)];
+    const int n0 = blockIdx.y * 64, b0 = blockIdx.x * 64;
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;    // 4 columns, 16 rows a pass
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = n0 + i * 16 + y, c = b0 + 4 * x;
+        if (n >= N || c >= cols) continue;
+        const float rn = r[n];
+        f32x4_t s = *reinterpret_cast<const f32x4_t*>(S + (int64_t)n * lds + c);
+        const float ls = lse[n];
+        const int64_t at = labels ? labels[n] - c0 - c : -1;
+        E g[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float v = exp_f(s[e] * inv_t - ls);
+            if (at == e) v -= 1.f;
+            // a token without a target: 0 whatever its logits are
+            g[e] = to_elem(rn == 0.f ? 0.f : rn * v, E());
+            tile[i * 16 + y][4 * x + e] = g[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < cols) G[(int64_t)n * ldg + c + e] = g[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = b0 + i * 16 + y, n = n0 + 4 * x;
+        if (c >= cols) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < N) GT[(int64_t)c * ldgt + n + e] = tile[4 * x + e][i * 16 + y];
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void fix_kernel(LossTargets t, const float* __restrict__ picked, int64_t ldpk,
+                                                  const float* __restrict__ lse, const float* __restrict__ r,
+                                                  int64_t total, int c0, int cols, E* __restrict__ G, int64_t ldg,
+                                                  E* __restrict__ GT, int64_t ldgt) {
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= total) return;
+    const int c = t.col[at] - c0;
+    if (t.col[at] < 0 || c < 0 || c >= cols) return;
+    const int n = (int)(at / t.T), j = (int)(at - (int64_t)n * t.T);
+    const float rn = r[n];
+    if (rn == 0.f) return;
+    const E g = to_elem(rn * (exp_f(picked[(int64_t)n * ldpk + j] - lse[n]) - t.p[at]), E());
+    G[(int64_t)n * ldg + c] = g;
+    GT[(int64_t)c * ldgt + n] = g;
+}
+
+__device__ __forceinline__ uint16_t zero_of(uint16_t) { return 0; }
+__device__ __forceinline__ float zero_of(float) { return 0.f; }
+
+template <typename E>
+__global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict__ X, int64_t ldx,
+                                                             const float* __restrict__ r, int N, int K,
+                                                             E* __restrict__ dst, int64_t ldd) {
+    __shared__ E tile[64][64 + 4 / sizeof(E)];
+    const int n0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int n = n0 + i * 4 + y, k = k0 + x;
+        E v = zero_of(E());
+        if (n < N && k < K && r[n] != 0.f) v = X[(int64_t)n * ldx + k];
+        tile[i * 4 + y][x] = v;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int k = k0 + i * 4 + y, n = n0 + x;
+        if (k < K && n < N) dst[(int64_t)k * ldd + n] = tile[x][i * 4 + y];
+    }
+}
+
+__global__ __launch_bounds__(256) void add_f32_kernel(f32x4_t* __restrict__ acc, const f32x4_t* __restrict__ src,
+                                                      int64_t quads) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (int64_t)gridDim.x * 256)
+        acc[i] += src[i];
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void scale_out_kernel(const float* __restrict__ src, int64_t lds,
+                                                        const float* __restrict__ scale, E* __restrict__ out,
+                                                        int64_t ldo, int64_t R, int64_t C) {
+    const float a = scale[0];
+    const int64_t quads = (C + 3) / 4, total = R * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / quads, c = (i - row * quads) * 4;
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(src + row * lds + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < C) out[row * ldo + c + e] = to_elem(a * v[e], E());
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void zero_kernel(E* __restrict__ out, int64_t ldo, int64_t R, int64_t C) {
+    const int64_t total = R * C;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256)
+        out[i / C * ldo + i % C] = zero_of(E());
+}
+
+unsigned blocks_of(int64_t items, int64_t most = 16384) {
+    const int64_t b = (items + 255) / 256;
+    return (unsigned)(b < 1 ? 1 : (b < most ? b : most));
+}
+
+}  // namespace
+
+hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits, int64_t ldl, int N, int T, int V,
+                          float inv_t, bool merge, int* col, float* p, float* logp, float* mass, hipStream_t stream) {
+    const dim3 grid((N + 3) / 4), block(256);
+#define TEACHER(U)                                                                                                  \
+    hipLaunchKernelGGL(teacher_kernel<U>, grid, block, 0, stream, index, ldi, logits, ldl, N, T, V, inv_t, merge ? 1 : 0, \
+                       col, p, logp, mass)
+    if (T <= 64) TEACHER(1);
+    else if (T <= 128) TEACHER(2);
+    else if (T <= 256) TEACHER(4);
+    else if (T <= 512) TEACHER(8);
+    else TEACHER(16);
+#undef TEACHER
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_stats(const float* S, int64_t lds, int N, int c0, int cols, float inv_t,
+                             const LossTargets& t, float2* part, int ldpart, int part0, float* picked, int64_t ldpk,
+                             hipStream_t stream) {
+    // a launch has at most 65535 workgroups in y
+    const int chunks = (cols + STAT_COLS - 1) / STAT_COLS;
+    for (int n0 = 0; n0 < N; n0 += 65535) {
+        const int rows = N - n0 < 65535 ? N - n0 : 65535;
+        LossTargets u = t;
+        if (u.labels) u.labels += n0;
+        if (u.col) u.col += (int64_t)n0 * t.T;
+        hipLaunchKernelGGL(stats_kernel, dim3(chunks, rows), dim3(256), 0, stream, S + (int64_t)n0 * lds, lds, c0, cols,
+                           inv_t, u, part + (int64_t)n0 * ldpart, ldpart, part0, picked + (int64_t)n0 * ldpk, ldpk);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_finish(const float2* part, int ldpart, int nparts, int N, int V, float temperature, const LossTargets& t,
+                              float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream) {
+    hipLaunchKernelGGL(finish_kernel, dim3((N + 3) / 4), dim3(256), 0, stream, part, ldpart, nparts, N, V,
+                       temperature * temperature, t, picked, ldpk, loss, lse);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
+                            float* r, float* scale, hipStream_t stream) {
+    hipLaunchKernelGGL(coef_kernel, dim3(1), dim3(1024), 0, stream, dloss, labels, mass, t, N, V, r, scale);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_grad(const float* S, int64_t lds, int N, int c0, int cols, float inv_t, const float* lse,
+                            const float* r, const int64_t* labels, void* G, int64_t ldg, void* GT, int64_t ldgt,
+                            bool f32, hipStream_t stream) {
+    const int tc = (cols + 63) / 64;
+    for (int n0 = 0; n0 < N; n0 += 65535 * 64) {
+        const int rows = N - n0 < 65535 * 64 ? N - n0 : 65535 * 64;
+        const dim3 grid(tc, (rows + 63) / 64), block(256);
+        if (f32)
+            hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S + (int64_t)n0 * lds, lds, rows, c0, cols,
+                               inv_t, lse + n0, r + n0, labels ? labels + n0 : nullptr, (float*)G + (int64_t)n0 * ldg,
+                               ldg, (float*)GT + n0, ldgt);
+        else
+            hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S + (int64_t)n0 * lds, lds, rows, c0,
+                               cols, inv_t, lse + n0, r + n0, labels ? labels + n0 : nullptr,
+                               (uint16_t*)G + (int64_t)n0 * ldg, ldg, (uint16_t*)GT + n0, ldgt);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ldpk, const float* lse, const float* r,
+                           int N, int c0, int cols, void* G, int64_t ldg, void* GT, int64_t ldgt, bool f32,
+                           hipStream_t stream) {
+    const int64_t total = (int64_t)N * t.T;
+    const dim3 grid((unsigned)((total + 255) / 256)), block(256);
+    if (f32)
+        hipLaunchKernelGGL(fix_kernel<float>, grid, block, 0, stream, t, picked, ldpk, lse, r, total, c0, cols,
+                           (float*)G, ldg, (float*)GT, ldgt);
+    else
+        hipLaunchKernelGGL(fix_kernel<uint16_t>, grid, block, 0, stream, t, picked, ldpk, lse, r, total, c0, cols,
+                           (uint16_t*)G, ldg, (uint16_t*)GT, ldgt);
+    return hipGetLastError();
+}
+
+hipError_t launch_transpose_live(const void* X, int64_t ldx, const float* r, int N, int K, void* dst, int64_t ldd,
+                                 bool f32, hipStream_t stream) {
+    // at most 65535 workgroups in y
+    for (int k0 = 0; k0 < K; k0 += 65535 * 64) {
+        const int k = K - k0 < 65535 * 64 ? K - k0 : 65535 * 64;
+        const dim3 grid((N + 63) / 64, (k + 63) / 64), block(256);
+        if (f32)
+            hipLaunchKernelGGL(transpose_live_kernel<float>, grid, block, 0, stream, (const float*)X + k0, ldx, r, N, k,
+                               (float*)dst + (int64_t)k0 * ldd, ldd);
+        else
+            hipLaunchKernelGGL(transpose_live_kernel<uint16_t>, grid, block, 0, stream, (const uint16_t*)X + k0, ldx, r,
+                               N, k, (uint16_t*)dst + (int64_t)k0 * ldd, ldd);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_add_f32(float* acc, const float* src, int64_t elems, hipStream_t stream) {
+    hipLaunchKernelGGL(add_f32_kernel, dim3(blocks_of(elems / 4)), dim3(256), 0, stream, (f32x4_t*)acc,
+                       (const f32x4_t*)src, elems / 4);
+    return hipGetLastError();
+}
+
+hipError_t launch_scale_out(const float* src, int64_t lds, const float* scale, void* out, int64_t ldo, int64_t R,
+                            int64_t C, bool f32, hipStream_t stream) {
+    const dim3 grid(blocks_of(R * ((C + 3) / 4))), block(256);
+    if (f32)
+        hipLaunchKernelGGL(scale_out_kernel<float>, grid, block, 0, stream, src, lds, scale, (float*)out, ldo, R, C);
+    else
+        hipLaunchKernelGGL(scale_out_kernel<uint16_t>, grid, block, 0, stream, src, lds, scale, (uint16_t*)out, ldo, R,
+                           C);
+    return hipGetLastError();
+}
+
+hipError_t launch_zero(void* out, int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream) {
+    const dim3 grid(blocks_of(R * C)), block(256);
+    if (f32) hipLaunchKernelGGL(zero_kernel<float>, grid, block, 0, stream, (float*)out, ldo, R, C);
+    else hipLaunchKernelGGL(zero_kernel<uint16_t>, grid, block, 0, stream, (uint16_t*)out, ldo, R, C);
+    return hipGetLastError();
+}
+
+}  // namespace espace

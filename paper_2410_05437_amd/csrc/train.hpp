@@ -1,0 +1,74 @@
+// Host-side launchers of the losses' and the embedding's kernels (internal to the
+// library).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace espace {
+
+// The targets of N tokens: one label each (labels), or T entries each (col, p; col
+// < 0: none) that launch_teacher made.
+struct LossTargets {
+    const int64_t* labels = nullptr;
+    const int* col = nullptr;
+    const float* p = nullptr;
+    const float* logp = nullptr;
+    int T = 1;
+};
+
+// Columns of S that one workgroup of launch_loss_stats reduces.
+constexpr int STAT_COLS = 4096;
+
+// The teacher's distributions: col[n][j] its entry (-1: empty), p[n][j], logp[n][j].
+// merge: an entry that occurs again is added to its first place, whose other places
+// become empty, and mass[n] is 1, or 0 for a token without a target.
+hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits, int64_t ldl, int N, int T, int V,
+                          float inv_t, bool merge, int* col, float* p, float* logp, float* mass, hipStream_t stream);
+
+// Columns [c0, c0 + cols) of the logits, S [N][lds] float32: the largest s / t and Σ
+// exp(s / t - it) of every STAT_COLS of them at part[n][part0 ...], and s / t of the
+// targets among them at picked[n][j].
+hipError_t launch_loss_stats(const float* S, int64_t lds, int N, int c0, int cols, float inv_t,
+                             const LossTargets& t, float2* part, int ldpart, int part0, float* picked, int64_t ldpk,
+                             hipStream_t stream);
+// loss and lse from nparts parts of each token (rows ldpart apart); picked of empty
+// places.
+hipError_t launch_loss_finish(const float2* part, int ldpart, int nparts, int N, int V, float temperature, const LossTargets& t,
+                              float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream);
+
+// r[n] = coef[n] / c and scale[0] = c, with coef the factor of token n's row of G (0
+// without a target) and c the largest of their magnitudes.
+hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
+                            float* r, float* scale, hipStream_t stream);
+// G [N][ldg] and its transpose GT [cols][ldgt] of columns [c0, c0 + cols) from S
+// (type f32 or bfloat16); labels may be NULL (their entries are launch_loss_fix's).
+hipError_t launch_loss_grad(const float* S, int64_t lds, int N, int c0, int cols, float inv_t, const float* lse,
+                            const float* r, const int64_t* labels, void* G, int64_t ldg, void* GT, int64_t ldgt,
+                            bool f32, hipStream_t stream);
+// The teacher's entries among these columns, from their logits `picked`.
+hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ldpk, const float* lse, const float* r,
+                           int N, int c0, int cols, void* G, int64_t ldg, void* GT, int64_t ldgt, bool f32,
+                           hipStream_t stream);
+// dst[k][n] = X[n][k], 0 where r[n] is 0.
+hipError_t launch_transpose_live(const void* X, int64_t ldx, const float* r, int N, int K, void* dst, int64_t ldd,
+                                 bool f32, hipStream_t stream);
+// acc += src (rows of ld elements, a multiple of 4)
+hipError_t launch_add_f32(float* acc, const float* src, int64_t elems, hipStream_t stream);
+// out[r][c] = scale[0]·src[r][c]
+hipError_t launch_scale_out(const float* src, int64_t lds, const float* scale, void* out, int64_t ldo, int64_t R,
+                            int64_t C, bool f32, hipStream_t stream);
+
+// zeros in the columns [0, C) of R rows
+hipError_t launch_zero(void* out, int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream);
+
+// ---- embedding -----------------------------------------------------------------
+hipError_t launch_embedding(const int64_t* tokens, const void* E, int64_t lde, void* X, int64_t ldx, int64_t N,
+                            int64_t K, int64_t V, float scale, bool f32, hipStream_t stream);
+size_t embedding_workspace_bytes(int64_t N, int64_t K, int64_t V);
+hipError_t launch_embedding_backward(const int64_t* tokens, const void* dX, int64_t lddx, void* dE, int64_t ldde,
+                                     int64_t N, int64_t K, int64_t V, float scale, bool accumulate, bool f32,
+                                     void* workspace, hipStream_t stream);
+
+}  // namespace espace

@@ -1,0 +1,181 @@
+"""espace_train.h without a GPU: exports, refusals before any device call, workspace
+sizes, and the binding's checks."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2410_05437_amd as E
+from paper_2410_05437_amd import _lib
+
+L = E.lib
+NULL = ctypes.c_void_p(0)
+BIG = (1 << 64) - 1
+
+
+def P(i):
+    """Made-up pointers 256 MB apart, 256-byte aligned; never dereferenced."""
+    return ctypes.c_void_p(i << 28)
+
+
+def off(p, n):
+    return ctypes.c_void_p(p.value + n)
+
+
+def test_exports():
+    names = E.header_functions(_lib.TRAIN_HEADER)
+    assert set(names) == {
+        "espace_linear_cross_entropy", "espace_linear_cross_entropy_backward", "espace_linear_distillation",
+        "espace_linear_distillation_backward", "espace_linear_loss_workspace_bytes", "espace_embedding",
+        "espace_embedding_backward", "espace_embedding_workspace_bytes"}
+    for n in names:
+        assert hasattr(L, n) and hasattr(E, n)
+
+
+def _ce(X=P(1), ldx=64, W=P(2), ldw=64, labels=P(3), loss=P(4), lse=P(5), N=8, K=64, V=100, dt=1, ws=P(9), wsb=1 << 24):
+    return L.espace_linear_cross_entropy(X, ldx, W, ldw, labels, loss, lse, N, K, V, dt, ws, wsb, NULL)
+
+
+def _ceb(dloss=P(6), X=P(1), ldx=64, W=P(2), ldw=64, labels=P(3), lse=P(5), dX=P(7), lddx=64, dW=P(8), lddw=64, N=8, K=64,
+         V=100, dt=1, ws=P(9), wsb=1 << 24):
+    return L.espace_linear_cross_entropy_backward(dloss, X, ldx, W, ldw, labels, lse, dX, lddx, dW, lddw, N, K, V, dt, ws,
+                                                  wsb, NULL)
+
+
+def _kd(X=P(1), ldx=64, W=P(2), ldw=64, index=P(3), ldi=4, logits=P(10), ldl=4, loss=P(4), lse=P(5), picked=P(11), ldpk=4,
+        N=8, K=64, V=100, T=4, t=2.0, dt=1, ws=P(9), wsb=1 << 24):
+    return L.espace_linear_distillation(X, ldx, W, ldw, index, ldi, logits, ldl, loss, lse, picked, ldpk, N, K, V, T, t, dt,
+                                        ws, wsb, NULL)
+
+
+def _kdb(dloss=P(6), X=P(1), ldx=64, W=P(2), ldw=64, index=P(3), ldi=4, logits=P(10), ldl=4, lse=P(5), picked=P(11), ldpk=4,
+         dX=P(7), lddx=64, dW=P(8), lddw=64, N=8, K=64, V=100, T=4, t=2.0, dt=1, ws=P(9), wsb=1 << 24):
+    return L.espace_linear_distillation_backward(dloss, X, ldx, W, ldw, index, ldi, logits, ldl, lse, picked, ldpk, dX, lddx,
+                                                 dW, lddw, N, K, V, T, t, dt, ws, wsb, NULL)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="valid calls with made-up pointers")
+def test_valid_calls_reach_the_device():
+    for s in (_ce(), _ce(dt=0), _ceb(), _ceb(dX=NULL), _ceb(dW=NULL), _kd(), _kd(T=1, ldi=7), _kdb(), _kdb(dX=NULL)):
+        assert s in (7, 8), L.espace_last_error()
+
+
+def test_loss_refusals():
+    for call in (_ce, _ceb, _kd, _kdb):
+        assert call(X=NULL) == 1 and call(W=NULL) == 1 and call(lse=NULL) == 1
+        assert call(N=-1) == 2 and call(N=1 << 22) == 2 and call(K=0) == 2 and call(V=0) == 2 and call(V=1 << 31) == 2
+        assert call(ldx=56) == 2 and call(ldw=56) == 2 and call(ldx=68) == 3
+        assert call(X=off(P(1), 8)) == 3 and call(lse=off(P(5), 2)) == 3
+        assert call(dt=2) == 4
+        assert call(ws=NULL) == 6 and call(wsb=256) == 6 and call(ws=off(P(9), 16)) == 3
+        assert call(ws=P(1)) == 5 and call(ws=off(P(2), 1024)) == 5
+    assert _ce(labels=NULL) == 1 and _ce(labels=off(P(3), 4)) == 3 and _ce(loss=NULL) == 1
+    assert _ce(loss=P(5)) == 5 and _ce(loss=off(P(1), 64)) == 5 and _ce(lse=off(P(3), 8)) == 5 and _ce(loss=off(P(9), 0)) == 5
+    assert _ceb(dloss=NULL) == 1 and _ceb(lddx=56) == 2 and _ceb(dX=off(P(8), 128)) == 5 and _ceb(dW=P(2)) == 5
+    assert _ceb(dX=off(P(5), 0)) == 5 and _ceb(dW=off(P(6), 0)) == 5
+    for call in (_kd, _kdb):
+        assert call(index=NULL) == 1 and call(logits=NULL) == 1 and call(picked=NULL) == 1
+        assert call(ldi=3) == 2 and call(ldl=3) == 2 and call(ldpk=3) == 2
+        assert call(T=0) == 2 and call(T=1025) == 2
+        for t in (0.0, -1.0, float("nan"), float("inf"), 1e-39, 1e30):
+            assert call(t=t) == 2
+        assert call(index=off(P(3), 4)) == 3 and call(picked=off(P(11), 2)) == 3
+    assert _kd(picked=off(P(10), 16)) == 5 and _kd(picked=P(4)) == 5
+    assert _kdb(dX=P(11)) == 5
+    assert "overlaps" in L.espace_last_error().decode()
+
+
+def test_nothing_to_do():
+    assert _ce(N=0, X=NULL, W=NULL, labels=NULL, loss=NULL, lse=NULL, ws=NULL, wsb=0) == 0
+    assert _kd(N=0, X=NULL, W=NULL, index=NULL, logits=NULL, picked=NULL, ws=NULL, wsb=0) == 0
+    assert _ceb(dX=NULL, dW=NULL, X=NULL, W=NULL, ws=NULL, wsb=0) == 0
+    assert _ceb(N=0, dW=NULL, X=NULL, W=NULL, labels=NULL, dloss=NULL, lse=NULL, ws=NULL, wsb=0) == 0
+    assert L.espace_embedding(NULL, NULL, 64, NULL, 64, 0, 64, 10, 1.0, 1, NULL) == 0
+    assert L.espace_embedding_backward(NULL, NULL, 64, P(2), 64, 0, 64, 10, 1.0, 1, 1, NULL, 0, NULL) == 0
+
+
+def test_loss_workspace_sizes():
+    ws = L.espace_linear_loss_workspace_bytes
+    for b in (0, 1):
+        assert ws(b, 0, 64, 100, 0, 1) == 0
+        assert ws(b, -1, 64, 100, 0, 1) == BIG and ws(b, 1 << 22, 64, 100, 0, 1) == BIG
+        assert ws(b, 8, 0, 100, 0, 1) == BIG and ws(b, 8, 64, 0, 0, 1) == BIG
+        assert ws(b, 8, 64, 100, -1, 1) == BIG and ws(b, 8, 64, 100, 1025, 1) == BIG and ws(b, 8, 64, 100, 4, 5) == BIG
+        assert 0 < ws(b, 8, 64, 100, 0, 0) < ws(b, 8, 64, 100, 4, 0)
+    # the logits of 8192 tokens over 50257 entries are 1.6 GB
+    assert ws(0, 8192, 6144, 50257, 0, 1) < 400 << 20
+    assert ws(1, 8192, 6144, 50257, 0, 1) < 1200 << 20
+
+
+def _emb(tokens=P(1), e=P(2), lde=64, X=P(3), ldx=64, N=8, K=64, V=100, dt=1):
+    return L.espace_embedding(tokens, e, lde, X, ldx, N, K, V, 1.0, dt, NULL)
+
+
+def _embb(tokens=P(1), dX=P(2), lddx=64, dE=P(3), ldde=64, N=8, K=64, V=100, acc=0, dt=1, ws=P(4), wsb=1 << 20):
+    return L.espace_embedding_backward(tokens, dX, lddx, dE, ldde, N, K, V, 1.0, acc, dt, ws, wsb, NULL)
+
+
+def test_embedding_refusals():
+    assert _emb(tokens=NULL) == 1 and _emb(e=NULL) == 1 and _emb(X=NULL) == 1
+    assert _emb(N=-1) == 2 and _emb(N=1 << 22) == 2 and _emb(K=0) == 2 and _emb(V=0) == 2
+    assert _emb(lde=56) == 2 and _emb(ldx=60) == 2 and _emb(ldx=68) == 3 and _emb(tokens=off(P(1), 4)) == 3
+    assert _emb(dt=9) == 4 and _emb(X=off(P(2), 128)) == 5 and _emb(X=P(1)) == 5
+    assert _embb(tokens=NULL) == 1 and _embb(dX=NULL) == 1 and _embb(dE=NULL) == 1
+    assert _embb(N=1 << 22) == 2 and _embb(K=0) == 2 and _embb(V=0) == 2 and _embb(ldde=56) == 2 and _embb(lddx=65) == 3
+    assert _embb(dt=-1) == 4 and _embb(dE=off(P(2), 128)) == 5 and _embb(ws=P(2)) == 5 and _embb(ws=P(3)) == 5
+    assert _embb(ws=NULL) == 6 and _embb(wsb=64) == 6 and _embb(ws=off(P(4), 8)) == 3
+    assert L.espace_embedding_workspace_bytes(-1, 64, 100) == BIG
+    assert L.espace_embedding_workspace_bytes(8, 64, 0) == BIG
+    assert L.espace_embedding_workspace_bytes(0, 64, 100) == 0
+    if not torch.cuda.is_available():
+        assert _emb() in (7, 8) and _embb() in (7, 8) and _embb(acc=1) in (7, 8)
+
+
+def test_the_bindings_checks():
+    bf, f32, i64 = torch.bfloat16, torch.float32, torch.int64
+    X, W, lab = torch.zeros(4, 16, dtype=bf), torch.zeros(9, 16, dtype=bf), torch.zeros(4, dtype=i64)
+    v, idx, z = torch.zeros(4), torch.zeros(4, 2, dtype=i64), torch.zeros(4, 2)
+    with pytest.raises(TypeError, match="W"):
+        E.espace_linear_cross_entropy(X, W.float(), lab)
+    with pytest.raises(ValueError, match="X"):
+        E.espace_linear_cross_entropy(X, W[:, :8], lab)
+    with pytest.raises(TypeError, match="labels"):
+        E.espace_linear_cross_entropy(X, W, lab.int())
+    with pytest.raises(ValueError, match="labels"):
+        E.espace_linear_cross_entropy(X, W, torch.zeros(5, dtype=i64))
+    with pytest.raises(ValueError, match="labels"):
+        E.espace_linear_cross_entropy(X, W, torch.zeros(8, dtype=i64)[::2])
+    with pytest.raises(TypeError, match="loss"):
+        E.espace_linear_cross_entropy(X, W, lab, loss=v.double())
+    with pytest.raises(ValueError, match="dloss"):
+        E.espace_linear_cross_entropy_backward(torch.ones(()).expand(4), X, W, lab, v)
+    with pytest.raises(TypeError, match="dloss"):
+        E.espace_linear_cross_entropy_backward(v.to(bf), X, W, lab, v)
+    with pytest.raises(TypeError, match="dX"):
+        E.espace_linear_cross_entropy_backward(v, X, W, lab, v, dX=torch.zeros(4, 16))
+    with pytest.raises(ValueError, match="dW"):
+        E.espace_linear_cross_entropy_backward(v, X, W, lab, v, dW=torch.zeros(9, 8, dtype=bf))
+    with pytest.raises(TypeError, match="logits"):
+        E.espace_linear_distillation(X, W, idx, z.to(bf))
+    with pytest.raises(ValueError, match="index"):
+        E.espace_linear_distillation(X, W, lab, z)
+    with pytest.raises(ValueError, match="logits"):
+        E.espace_linear_distillation(X, W, idx, torch.zeros(4, 3))
+    with pytest.raises(ValueError, match="column stride"):
+        E.espace_linear_distillation(X, W, idx, torch.zeros(2, 4).t())
+    with pytest.raises(ValueError, match="picked"):
+        E.espace_linear_distillation_backward(v, X, W, idx, z, v, torch.zeros(4, 3))
+    with pytest.raises(TypeError, match="tokens"):
+        E.espace_embedding(lab.int(), W)
+    with pytest.raises(ValueError, match="X"):
+        E.espace_embedding(lab, W, X=torch.zeros(4, 8, dtype=bf))
+    with pytest.raises(ValueError, match="accumulate"):
+        E.espace_embedding_backward(lab, X, 9, accumulate=True)
+    with pytest.raises(TypeError, match="dE"):
+        E.espace_embedding_backward(lab, X, 9, dE=torch.zeros(9, 16))
+    with pytest.raises(ValueError, match="tokens"):
+        E.espace_embedding_backward(lab[:3], X, 9)
+    with pytest.raises(E.EspaceError):
+        E.espace_linear_loss_workspace_bytes(True, 4, 16, 9, 2000, bf)
+    with pytest.raises(E.EspaceError):
+        E.espace_embedding_workspace_bytes(1 << 23, 16, 9)
