@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "kernels.hpp"
+
 namespace espace {
 namespace api {
 
@@ -23,6 +25,9 @@ size_t align_ws(size_t x);
 
 // Compute units of the current device.
 int device_cus();
+
+// ESPACE_PLAN_LOG=1 prints each product's plan to stderr (read once per process).
+bool plan_log();
 
 // An operand's addresses, for the check that no output overlaps it.
 struct Range { const char* name; uintptr_t lo, hi; };
@@ -41,9 +46,18 @@ espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, voi
                      int64_t Cc, int64_t D, espace_dtype dt, void* partial, hipStream_t stream);
 
 // The same with C in float32 whatever the operands' type, ldc = splitk_ld(Cc) and C
-// the library's own scratch: columns up to ldc may be written.  Needs no partial sums.
+// the library's own scratch: columns up to ldc may be written.  Needs no partial
+// sums.  ranges > 1 (bfloat16): the sums of up to so many depth ranges, *made of them,
+// R·ldc apart in C, not combined.
 espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
-                         int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream);
+                         int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream, int ranges = 1,
+                         int* made = nullptr);
+// bfloat16: the tile (256 x 256 or 256 x 192) that run_tn_f32 takes in one range, or -1
+// where another kernel is priced below these or takes the sizes.
+int f32_tile(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb);
+// A product of a loss (LossEpi) on such a tile.
+espace_status run_tn_loss(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R,
+                          int64_t Cc, int64_t D, int tile, LossMode mode, const LossEpi& epi, hipStream_t stream);
 
 #define ESPACE_TRY(x)                       \
     do {                                    \

@@ -744,59 +744,101 @@ size_t run_tn_partial_bytes(int64_t R, int64_t Cc, int64_t D, espace_dtype dt) {
     return plan_tn(R, Cc, D, dt).partial_bytes;
 }
 
-espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
-                         int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream) {
-    hipError_t e;
+namespace {
+
+GemmArgs f32_args(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R, int64_t Cc,
+                  int64_t D) {
+    GemmArgs g{};
+    g.A = (const uint16_t*)A;
+    g.lda = lda;
+    g.B = (const uint16_t*)B;
+    g.ldb = ldb;
+    g.C = C;
+    g.ldc = ldc;
+    g.R = (int)R;
+    g.Cc = (int)Cc;
+    g.D = (int)D;
+    g.c_f32 = 1;
+    g.splits = 1;
+    g.partial = (float*)C;
+    g.cus = device_cus();
+    g.wait = wait_cfg();
+    return g;
+}
+
+}  // namespace
+
+// The cheapest of 256 x 256 and 256 x 192 tiles, priced as in plan_tiled_one, and the
+// small tiles, with up to `ranges` depth ranges.  tile -1: small tiles (config).
+struct F32Plan { int tile = -1, config = 0, ranges = 1; };
+
+static F32Plan f32_plan(int R, int Cc, int D, int64_t lda, int64_t ldb, int ranges) {
+    const int64_t lim = (int64_t)1 << 31;
     const int cus = device_cus();
+    const double byte_cost = 315.0 / (2.0 * 64 * cus);
+    F32Plan p;
+    double best = 1e300;
+    if (espace::mid_supported(lda, ldb)) best = espace::mid_plan(R, Cc, D, cus, ranges, &p.config, &p.ranges);
+    if (R * lda >= lim || Cc * ldb >= lim) return p;
+    const int ktiles = ceil_div(D, 64);
+    for (const int bn : {256, 192})
+        for (int s = 1; s <= ranges && (s == 1 || ktiles / s >= 8); ++s) {
+            const int64_t rounds = ceil_div((int64_t)ceil_div(R, 256) * ceil_div(Cc, bn) * s, cus);
+            double c = rounds * (256.0 * bn * ceil_div(ktiles, s) / (bn == 256 ? 1.0 : 0.933) + 101e3);
+            if (s > 1) c += 97e3 + 1.37 * s * (double)R * Cc * 4.0 * byte_cost;
+            if (4.75 + kUnitUs * c >= best) continue;
+            best = 4.75 + kUnitUs * c;
+            p.tile = bn == 256 ? espace::TILE_256x256 : espace::TILE_256x192;
+            p.ranges = s;
+        }
+    return p;
+}
+
+int f32_tile(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb) {
+    if (use_gemv((int)R, (int)Cc, (int)D)) return -1;
+    return f32_plan((int)R, (int)Cc, (int)D, lda, ldb, 1).tile;
+}
+
+espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
+                         int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream, int ranges, int* made) {
+    hipError_t e;
+    int one = 1;
+    if (!made) made = &one;
+    *made = 1;
     if (dt == ESPACE_F32) {
         e = espace::launch_gemm_tn_f32((const float*)A, lda, (const float*)B, ldb, C, ldc, (int)R, (int)Cc, (int)D,
-                                       cus, stream);
+                                       device_cus(), stream);
     } else {
-        GemmArgs g{};
-        g.A = (const uint16_t*)A;
-        g.lda = lda;
-        g.B = (const uint16_t*)B;
-        g.ldb = ldb;
-        g.C = C;
-        g.ldc = ldc;
-        g.R = (int)R;
-        g.Cc = (int)Cc;
-        g.D = (int)D;
-        g.c_f32 = 1;
-        g.splits = 1;
-        g.partial = C;
-        g.cus = cus;
-        const int64_t lim = (int64_t)1 << 31;
-        double us = 0;
-        int config = 0, splits = 1;
+        GemmArgs g = f32_args(A, lda, B, ldb, C, ldc, R, Cc, D);
         if (use_gemv((int)R, (int)Cc, (int)D)) {
             e = espace::launch_gemv_tn_bf16(g, stream);
         } else {
-            // small tiles up to the token counts of plan_bf16, where they are priced
-            // below a 256 x 256 or 256 x 192 tile per round of workgroups
-            double tiled = 1e300;
-            for (const int bn : {256, 192}) {
-                const int64_t rounds = ceil_div((int64_t)ceil_div(R, 256) * ceil_div(Cc, bn), cus);
-                const double t = 4.75 + kUnitUs * rounds * (256.0 * bn * ceil_div(D, 64) / (bn == 256 ? 1.0 : 0.933) + 101e3);
-                if (t < tiled) {
-                    tiled = t;
-                    g.tile = bn == 256 ? espace::TILE_256x256 : espace::TILE_256x192;
-                }
-            }
-            if (R <= kMidMaxTokens) us = espace::mid_plan((int)R, (int)Cc, (int)D, cus, 1, &config, &splits);
-            if (R <= kMidMaxTokens && us < tiled && espace::mid_supported(lda, ldb)) {
-                g.tile = config;
+            const F32Plan p = f32_plan((int)R, (int)Cc, (int)D, lda, ldb, ranges);
+            g.splits = p.ranges;
+            if (p.tile >= 0) {
+                g.tile = p.tile;
+                e = espace::launch_gemm_tn_bf16_v3_ranges(g, false, made, stream);
+            } else if (espace::mid_supported(lda, ldb)) {
+                g.tile = p.config;
+                *made = p.ranges;
                 e = espace::launch_mid_tn_bf16(g, stream);
-            } else if (R * lda < lim && Cc * ldb < lim) {
-                int ranges = 1;
-                e = espace::launch_gemm_tn_bf16_v3_ranges(g, false, &ranges, stream);
             } else {
                 // matrices of 2^31 elements or more: the kernel with 64-bit offsets
                 g.tile = espace::TILE_128x128;
+                g.splits = 1;
                 e = espace::launch_gemm_tn_bf16(g, stream);
             }
         }
     }
+    if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
+    return ESPACE_OK;
+}
+
+espace_status run_tn_loss(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R,
+                          int64_t Cc, int64_t D, int tile, LossMode mode, const LossEpi& epi, hipStream_t stream) {
+    GemmArgs g = f32_args(A, lda, B, ldb, C, ldc, R, Cc, D);
+    g.tile = tile;
+    const hipError_t e = espace::launch_gemm_tn_bf16_loss(g, mode, epi, stream);
     if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
     return ESPACE_OK;
 }

@@ -36,6 +36,200 @@ namespace espace {
 
 namespace {
 
+struct V3NoEpi {};
+
+__device__ __forceinline__ float v3_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+
+// The rows of a wave's 128 x BN/2 sub-tile are spread as elsewhere: block (i, j), row
+// 16 i + lane % 16, columns 16 j + 4 (lane / 16) + {0..3}.  row0, col0: the sub-tile's
+// first row and column; slab: its index among the slabs of BN/2 columns.
+template <int MODE, int BN, class EPI>
+__device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3Cfg<BN>::NBJ], const EPI& epi,
+                                                 void* Cout, int64_t ldc, int row0, int col0, int slab, int R, int Cc,
+                                                 int lane, float* spare) {
+    constexpr int NBJ = V3Cfg<BN>::NBJ;
+    const int lr = lane & 15, lh = lane >> 4;
+    const int c0 = col0 + 4 * lh;                 // of block j: + 16 j
+    if constexpr (MODE == V3_STATS) {
+        const int entries = epi.T;
+        int lab[V3_NB];                           // the label's column in the sub-tile
+        int q0[V3_NB], q1[V3_NB];                 // the row's entries in the slab
+#pragma unroll
+        for (int i = 0; i < V3_NB; ++i) {
+            const int r = min(row0 + 16 * i + lr, R - 1);
+            lab[i] = -1;
+            q0[i] = q1[i] = 0;
+            if (epi.labels) {
+                const int64_t c = epi.labels[r] - epi.col0 - col0;
+                lab[i] = c >= 0 && c < BN / 2 && col0 + c < Cc ? (int)c : -1;
+            } else if (entries) {
+                const int at = epi.col0 / (BN / 2) + slab;
+                q0[i] = epi.first[(int64_t)r * epi.ldfirst + at];
+                q1[i] = epi.first[(int64_t)r * epi.ldfirst + at + 1];
+            }
+        }
+        // each of a row's four lanes looks at one entry at a time
+        int col[V3_NB];
+#pragma unroll
+        for (int i = 0; i < V3_NB; ++i) {
+            const int r = row0 + 16 * i + lr;
+            q0[i] += lh;
+            if (r >= R) q1[i] = 0;
+            col[i] = q0[i] < q1[i] ? epi.col[(int64_t)r * entries + q0[i]] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < V3_NB; ++i) {
+            const int r = row0 + 16 * i + lr;
+            float v[NBJ][4];
+            float m = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NBJ; ++j) {
+                const f32x4_t a = v3_acc_read(acc[i][j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[j][e] = c0 + 16 * j + e < Cc ? a[e] * epi.inv_t : -INFINITY;
+                    m = fmaxf(m, v[j][e]);
+                }
+            }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float base = m == -INFINITY ? 0.f : m;
+            float l = 0.f;
+#pragma unroll
+            for (int j = 0; j < NBJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l += v3_exp(v[j][e] - base);
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (lh == 0 && r < R) epi.part[(int64_t)slab * R + r] = make_float2(l == 0.f ? -INFINITY : base, l);
+            if (epi.labels) {
+                if (__any(lab[i] >= 0) && lab[i] >= 0 && r < R && ((lab[i] >> 2) & 3) == lh) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NBJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x = lab[i] == 16 * j + 4 * lh + e ? v[j][e] : x;
+                    epi.picked[(int64_t)r * epi.ldpk] = x;
+                }
+            } else if (entries && __any(q0[i] < q1[i])) {
+                // the wave's own LDS, in the order of its instructions; 16-byte chunk c
+                // of row r at chunk c ^ r, so that the 16 rows of a write lie on
+                // distinct banks
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < NBJ; ++j)
+                    *reinterpret_cast<f32x4_t*>(spare + lr * 128 + ((4 * j + lh) ^ lr) * 4) =
+                        f32x4_t{v[j][0], v[j][1], v[j][2], v[j][3]};
+                __builtin_amdgcn_wave_barrier();
+                int q = q0[i], c = col[i];
+                while (__any(q < q1[i])) {
+                    if (q < q1[i]) {
+                        const int at = min(max(c - epi.col0 - col0, 0), BN / 2 - 1);
+                        epi.picked[(int64_t)r * epi.ldpk + epi.place[(int64_t)r * entries + q]] =
+                            spare[lr * 128 + ((at >> 2) ^ lr) * 4 + (at & 3)];
+                    }
+                    q += 4;
+                    c = q < q1[i] ? epi.col[(int64_t)r * entries + q] : 0;
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    } else {
+        uint16_t* Cb = reinterpret_cast<uint16_t*>(Cout);
+        // as in the bf16 epilogue: 8 consecutive columns a lane, for 2 blocks of 16
+        const int cl0 = col0 + 16 * (lh & 1) + 8 * (lh >> 1);   // + 32 m
+        auto pack = [&](f32x4_t a, f32x4_t b) -> u32x4_t {
+            const auto s0 = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false,
+                                                             false);
+            const auto s1 = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[2], a[3]), pack_bf16x2(b[2], b[3]), false,
+                                                             false);
+            return u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+        };
+        if constexpr (MODE == V3_GRAD) {
+            const int Cc8 = (Cc + 7) & ~7;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Cb, (short)0,
+                                                                (int)(unsigned)((uint64_t)R * ldc * 2u), 0x00020000);
+            float ls[V3_NB], rn[V3_NB];
+            int lab[V3_NB];
+#pragma unroll
+            for (int i = 0; i < V3_NB; ++i) {
+                const int r = min(row0 + 16 * i + lr, R - 1);
+                ls[i] = epi.lse[r];
+                rn[i] = epi.r[r];
+                lab[i] = -1;
+                if (epi.labels) {
+                    const int64_t c = epi.labels[r] - epi.col0 - c0;
+                    lab[i] = c >= 0 && c < BN ? (int)c : -1;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < V3_NB; ++i) {
+                const int r = row0 + 16 * i + lr;
+                auto value = [&](int j) -> f32x4_t {
+                    const f32x4_t a = v3_acc_read(acc[i][j]);
+                    f32x4_t g;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float x = v3_exp(a[e] * epi.inv_t - ls[i]);
+                        x = lab[i] == 16 * j + e ? x - 1.f : x;
+                        // a token without a target: 0 whatever its logits are
+                        x = rn[i] == 0.f ? 0.f : rn[i] * x;
+                        g[e] = c0 + 16 * j + e < Cc ? x : 0.f;
+                    }
+                    return g;
+                };
+#pragma unroll
+                for (int m = 0; m < NBJ / 2; ++m) {
+                    const u32x4_t v = pack(value(2 * m), value(2 * m + 1));
+                    const int c = cl0 + 32 * m;
+                    const unsigned off =
+                        (r < R && c < Cc8) ? ((unsigned)r * (unsigned)ldc + (unsigned)c) * 2u : 0xFFFFFFF0u;
+                    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, (int)off, 0, 0);
+                }
+            }
+        } else {
+            const float a = epi.last ? epi.scale[0] : 1.f;
+#pragma unroll
+            for (int i = 0; i < V3_NB; ++i) {
+                const int r = row0 + 16 * i + lr;
+                float* row = epi.acc + (int64_t)min(r, R - 1) * epi.ldacc;
+                // rows of acc are padded to a multiple of 8 columns
+                f32x4_t before[NBJ];
+                if (epi.add) {
+#pragma unroll
+                    for (int j = 0; j < NBJ; ++j)
+                        before[j] = c0 + 16 * j < Cc ? *reinterpret_cast<const f32x4_t*>(row + c0 + 16 * j)
+                                                     : f32x4_t{0.f, 0.f, 0.f, 0.f};
+                }
+                auto value = [&](int j) -> f32x4_t {
+                    const f32x4_t x = v3_acc_read(acc[i][j]);
+                    return epi.add ? before[j] + x : x;
+                };
+                if (!epi.last) {
+#pragma unroll
+                    for (int j = 0; j < NBJ; ++j)
+                        if (r < R && c0 + 16 * j < Cc) *reinterpret_cast<f32x4_t*>(row + c0 + 16 * j) = value(j);
+                    continue;
+                }
+#pragma unroll
+                for (int m = 0; m < NBJ / 2; ++m) {
+                    const u32x4_t v = pack(value(2 * m) * a, value(2 * m + 1) * a);
+                    const int c = cl0 + 32 * m;
+                    if (r >= R) continue;
+                    uint16_t* p = Cb + (int64_t)r * ldc + c;
+                    if (c + 8 <= Cc) {
+                        *reinterpret_cast<u32x4_t*>(p) = v;
+                    } else if (c < Cc) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (c + e < Cc) p[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                    }
+                }
+            }
+        }
+    }
+}
+
 // Matrices handed to this kernel hold fewer than 2^31 elements (the launcher
 // checks), so byte offsets fit in 32 bits.  Every depth range is non-empty.
 //
@@ -51,18 +245,28 @@ namespace {
 // meet in v3_pair; `tile_state` and `pair_part` as there.  APAIR: A is in
 // the row-pair layout (pair_offset, lda its pair pitch); c_pairs: the bf16
 // output is written in that layout (ldc its pair pitch).
-template <int MODE, int BN, int APAIR = 0>
+//
+// MODE_STATS, MODE_GRAD, MODE_GRAD_OUT (EPI = LossEpi, which says what they write):
+// persistent like MODE_BF16.  Their epilogues read what belongs to the tile's rows,
+// so the wait for the next item's first step does not count on stores behind it
+// (ST = 0) and may wait for them as well.
+template <int MODE, int BN, int APAIR = 0, class EPI = V3NoEpi>
 __global__ __launch_bounds__(256, 1)
 void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
                             const uint16_t* __restrict__ B, int64_t ldb,
                             void* __restrict__ Cout, int64_t ldc,
                             int R, int Cc, int D, int tiles_c, int ntiles, int ktiles_per_split,
                             int64_t split_stride, int map, unsigned long long* tile_state,
-                            float* pair_part, unsigned long long epoch, WaitCfg wc, int c_pairs) {
+                            float* pair_part, unsigned long long epoch, WaitCfg wc, int c_pairs, EPI epi) {
     using C = V3Cfg<BN>;
     constexpr int NBJ = C::NBJ;
+    constexpr bool LOSS = MODE == V3_STATS || MODE == V3_GRAD || MODE == V3_GRAD_OUT;
+    constexpr int ST = LOSS ? 0 : C::NST;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM];
     __shared__ int pair_role;
+    // the sums of 16 rows of each wave, for entries at any column (MODE_STATS): all
+    // that the half-stages leave of the LDS
+    __shared__ __attribute__((aligned(16))) float spare[MODE == V3_STATS ? V3_NW * 16 * 128 : 1];
 
     const int ktiles = (D + V3_BK - 1) / V3_BK;
     const int kt0 = blockIdx.y * ktiles_per_split;
@@ -70,7 +274,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
     const int nfull = D / V3_BK < kt_end ? D / V3_BK : kt_end;   // end of the full-depth steps
     const int nsteps = kt_end - kt0;
     // the next item's first two steps can be loaded ahead
-    const bool ahead_ok = MODE == V3_BF16 && (Cc & 7) == 0 && kt0 + 2 <= nfull;
+    const bool ahead_ok = (LOSS || (MODE == V3_BF16 && (Cc & 7) == 0)) && kt0 + 2 <= nfull;
 
     // (one order in the symmetric product, where most panels are shared by many
     // XCDs: K = 4096, 8192 tokens 140 us, with an order per XCD 157)
@@ -121,7 +325,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         if (ahead) {
             // this wave's loads of the first step, then the loads of the second
             // and the previous item's stores were issued
-            v3_wait_vm<2 * C::LPH + C::NST>();
+            v3_wait_vm<2 * C::LPH + ST>();
         } else {
             // the half-stages may still be read by a wave finishing the previous item
             if (item != (int)blockIdx.x) __syncthreads();
@@ -171,7 +375,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
             constexpr bool F = decltype(first)::value;
             // after an item loaded ahead, its first step has the previous
             // item's stores in flight behind the loads of its second step
-            const int stores = (F && ahead) ? C::NST : 0;
+            const int stores = (F && ahead) ? ST : 0;
             // sub-step 0: fragments of sub-step 1 from the second half-stage
             int lkt;
             const int k0 = load_kind(0, lkt);
@@ -241,6 +445,10 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         // ---- epilogue ------------------------------------------------------------
         // block (i, j): lane holds output row wrow0 + 16 i + lr and the 4
         // columns wcol0 + 16 j + 4 lh + {0..3}
+        if constexpr (LOSS) {
+            v3_loss_epilogue<MODE, BN>(acc, epi, Cout, ldc, row0 + wrow0, col0 + wcol0,
+                                       (tile_c * BN + wcol0) / (BN / 2), R, Cc, lane, spare + (MODE == V3_STATS ? wave * 16 * 128 : 0));
+        } else {
         float* tpart = nullptr;
         unsigned long long* tstate = nullptr;
         bool timed_out = false;
@@ -366,6 +574,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
             if (threadIdx.x == 0) __hip_atomic_store(tstate, ((epoch & 0xFFFFFFFFFFFFull) << 16) | 3ull,
                                                      __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
+        }
         if (next >= ntiles) break;
         item = next;
         tile_r = ntr;
@@ -397,11 +606,11 @@ hipError_t launch_v3(const GemmArgs& g, hipStream_t stream) {
         if (g.a_pairs)
             hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_BF16, BN, 1>), grid, block, 0, stream, g.A, g.lda, g.B,
                                g.ldb, g.C, g.ldc, g.R, g.Cc, g.D, tiles_c, ntiles, ktps, (int64_t)0, map,
-                               nullptr, nullptr, 0ull, g.wait, g.c_pairs);
+                               nullptr, nullptr, 0ull, g.wait, g.c_pairs, V3NoEpi{});
         else
             hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_BF16, BN>), grid, block, 0, stream, g.A, g.lda, g.B,
                                g.ldb, g.C, g.ldc, g.R, g.Cc, g.D, tiles_c, ntiles, ktps, (int64_t)0, map,
-                               nullptr, nullptr, 0ull, g.wait, g.c_pairs);
+                               nullptr, nullptr, 0ull, g.wait, g.c_pairs, V3NoEpi{});
         return hipGetLastError();
     }
     dim3 grid(ntiles, S);
@@ -412,7 +621,7 @@ hipError_t launch_v3(const GemmArgs& g, hipStream_t stream) {
                 reinterpret_cast<unsigned long long*>(g.partial + (size_t)ntiles * V3_BM * BN);
             hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_PAIR, BN>), grid, block, 0, stream, g.A, g.lda, g.B,
                                g.ldb, g.C, g.ldc, g.R, g.Cc, g.D, tiles_c, ntiles, ktps, (int64_t)0, map,
-                               state, g.partial, g.epoch, g.wait, g.c_pairs);
+                               state, g.partial, g.epoch, g.wait, g.c_pairs, V3NoEpi{});
             return hipGetLastError();
         }
     }
@@ -420,7 +629,7 @@ hipError_t launch_v3(const GemmArgs& g, hipStream_t stream) {
     const int64_t split_stride = (int64_t)g.R * ldp;
     hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN>), grid, block, 0, stream, g.A, g.lda, g.B,
                        g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D, tiles_c, ntiles, ktps, split_stride,
-                       map, nullptr, nullptr, 0ull, g.wait, 0);
+                       map, nullptr, nullptr, 0ull, g.wait, 0, V3NoEpi{});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     return launch_splitk_reduce(g.partial, S, split_stride, ldp, g.C, g.ldc, g.R, g.Cc, g.c_pairs ? 2 : 1, stream);
@@ -439,11 +648,44 @@ hipError_t launch_v3_ranges(const GemmArgs& g, bool upper, int* ranges, hipStrea
     const int64_t ldp = splitk_ld(g.Cc);
     hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN>), dim3(ntiles, S), dim3(V3_NW * 64), 0, stream, g.A,
                        g.lda, g.B, g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D, tiles_c, ntiles, ktps,
-                       (int64_t)g.R * ldp, upper ? 8 : 0, nullptr, nullptr, 0ull, g.wait, 0);
+                       (int64_t)g.R * ldp, upper ? 8 : 0, nullptr, nullptr, 0ull, g.wait, 0, V3NoEpi{});
     return hipGetLastError();
 }
 
 }  // namespace
+
+template <int BN>
+static hipError_t launch_loss(const GemmArgs& g, LossMode mode, const LossEpi& epi, hipStream_t stream) {
+    const int tiles_c = (g.Cc + BN - 1) / BN;
+    const int ntiles = (g.R + V3_BM - 1) / V3_BM * tiles_c;
+    const int ktiles = (g.D + V3_BK - 1) / V3_BK;
+    const int persistent = g.cus > 0 ? g.cus : 256;
+    const dim3 grid(ntiles < persistent ? ntiles : persistent, 1), block(V3_NW * 64);
+    const int map = one_depth_order(g, V3_BM, BN) ? MAP_ONE_ORDER : 0;
+#define LAUNCH(MODE)                                                                                                  \
+    hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<MODE, BN, 0, LossEpi>), grid, block, 0, stream, g.A, g.lda, g.B, g.ldb, \
+                       g.C, g.ldc, g.R, g.Cc, g.D, tiles_c, ntiles, ktiles, (int64_t)0, map, nullptr, nullptr, 0ull,  \
+                       g.wait, 0, epi)
+    switch (mode) {
+        case LOSS_STATS: LAUNCH(V3_STATS); break;
+        case LOSS_GRAD: LAUNCH(V3_GRAD); break;
+        case LOSS_GRAD_OUT: LAUNCH(V3_GRAD_OUT); break;
+    }
+#undef LAUNCH
+    return hipGetLastError();
+}
+
+hipError_t launch_gemm_tn_bf16_loss(const GemmArgs& g, LossMode mode, const LossEpi& epi, hipStream_t stream) {
+    const int64_t lim = (int64_t)1 << 31;
+    if ((int64_t)g.R * g.lda >= lim || (int64_t)g.Cc * g.ldb >= lim || g.D < 1 ||
+        (mode == LOSS_GRAD && (int64_t)g.R * g.ldc >= lim))
+        return hipErrorInvalidValue;
+    switch (g.tile) {
+        case TILE_256x256: return launch_loss<256>(g, mode, epi, stream);
+        case TILE_256x192: return launch_loss<192>(g, mode, epi, stream);
+        default: return hipErrorInvalidValue;
+    }
+}
 
 hipError_t launch_gemm_tn_bf16_v3_ranges(const GemmArgs& g, bool upper, int* ranges, hipStream_t stream) {
     const int64_t lim = (int64_t)1 << 31;

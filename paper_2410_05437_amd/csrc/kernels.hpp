@@ -94,6 +94,41 @@ hipError_t launch_gemm_tn_bf16_v2(const GemmArgs& g, hipStream_t stream);
 // 2^31 elements or more.
 constexpr int V4_MIN_STEPS = 48;
 hipError_t launch_gemm_tn_bf16_v4(const GemmArgs& g, hipStream_t stream);
+// What a product of a loss on a head's logits does with its sums s (float32, columns
+// col0 on of the vocabulary):
+//  stats     nothing is written but, of each 128 columns (96 with 192-column tiles),
+//            the largest s·inv_t and Σ exp(s·inv_t - it) of every row, at part[k·R + row]
+//            for the k-th such slab, and s·inv_t of the targets
+//  grad      C = r[row]·(exp(s·inv_t - lse[row]) - [column = labels[row]]) in bfloat16,
+//            0 where r is 0, zeros up to a multiple of 8 columns
+//  grad_out  a gradient: acc (if add) + s is stored in acc, or times scale[0] in C
+//            in bfloat16 (if last)
+struct LossEpi {
+    float inv_t = 1.f;
+    int col0 = 0;
+    const int64_t* labels = nullptr;       // of the rows; NULL: entries, or none
+    float2* part = nullptr;
+    float* picked = nullptr;               // of labels: [row]; of entries: [row][entry]
+    int64_t ldpk = 1;
+    // T entries a row in the order of their columns (col) with their places (place)
+    // among the row's, and how many of them lie before each slab (first[row][slab])
+    const int* col = nullptr;
+    const uint16_t* place = nullptr;
+    const uint16_t* first = nullptr;
+    int64_t ldfirst = 0;
+    int T = 0;
+    const float* lse = nullptr;
+    const float* r = nullptr;
+    float* acc = nullptr;
+    int64_t ldacc = 0;
+    const float* scale = nullptr;
+    int add = 0, last = 0;
+};
+enum LossMode { LOSS_STATS, LOSS_GRAD, LOSS_GRAD_OUT };
+// 256 x 256 and 256 x 192 plans (g.tile) with these epilogues; loss_slab: the columns
+// of a slab of the tile.  hipErrorInvalidValue for matrices of 2^31 elements or more.
+inline int loss_slab(int tile) { return tile == TILE_256x192 ? 96 : 128; }
+hipError_t launch_gemm_tn_bf16_loss(const GemmArgs& g, LossMode mode, const LossEpi& epi, hipStream_t stream);
 // Four-wave 256 x 256 and 256 x 192 kernel with a hand-ordered main loop;
 // hipErrorInvalidValue for products it does not take (other tiles, fp32
 // output, >= 2^31 elements).
@@ -106,7 +141,8 @@ hipError_t launch_gemm_tn_bf16_v3(const GemmArgs& g, hipStream_t stream);
 double mid_plan(int R, int Cc, int D, int cus, int ranges, int* config, int* splits);
 int mid_waves(int config);
 bool mid_supported(int64_t lda, int64_t ldb);
-// c_f32: one range whose fp32 sums are the output (partial = C, ldc = splitk_ld(Cc))
+// c_f32: the fp32 sums of the ranges are the output, R * ldc apart (partial = C, ldc =
+// splitk_ld(Cc)); not combined
 hipError_t launch_mid_tn_bf16(const GemmArgs& g, hipStream_t stream);
 // Vector-ALU product for 1 <= R <= 2 tokens with whole-row streaming (tile,
 // splits, partial unused); gemv_supported says whether the tokens fit its LDS.

@@ -46,15 +46,16 @@ __device__ __forceinline__ float rescale(float l, float from, float to) {
 
 // ---- targets -------------------------------------------------------------------
 
-// One wave per token, entry 64 u + lane in register u.
+// One wave per token, entry 64 u + lane in register u.  An entry's rank among the
+// columns, and the sum of equal ones, come from T broadcasts of an entry to all (T
+// squared comparisons, 64 at a time: 64 entries 7 us for 4096 tokens).
 template <int U>
 __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict__ index, int64_t ldi,
                                                       const float* __restrict__ logits, int64_t ldl, int N, int T,
-                                                      int V, float inv_t, int merge, int* __restrict__ col,
-                                                      float* __restrict__ p_out, float* __restrict__ logp_out,
-                                                      float* __restrict__ mass) {
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+                                                      int V, float inv_t, TeacherOut out) {
+    __shared__ int lds_col[4][64 * U];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int n = blockIdx.x * 4 + wave;
     if (n >= N) return;
     int c[U];
     float z[U];
@@ -88,13 +89,14 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict_
         p[u] *= inv;
         lp[u] = z[u] == -INFINITY ? 0.f : (z[u] - m) - lg;
     }
-    if (merge) {
-        // every entry against all, in their order: the sum goes to the first place
+    if (out.sorted || out.mass) {
         float sum[U];
+        int rank[U];
         bool again[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             sum[u] = 0.f;
+            rank[u] = 0;
             again[u] = false;
         }
 #pragma unroll
@@ -104,27 +106,57 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict_
                 const float pk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p[v]), k));
                 const int j = 64 * v + k;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u) {
+                    const bool before = j < 64 * u + lane;
                     if (c[u] == ck) {
                         sum[u] += pk;
-                        again[u] |= j < 64 * u + lane;
+                        again[u] |= before;
                     }
+                    rank[u] += ck >= 0 && (ck < c[u] || (ck == c[u] && before));
+                }
             }
+        if (out.sorted) {
+            int there = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            p[u] = sum[u];
-            if (again[u]) c[u] = -1;
+            for (int u = 0; u < U; ++u) {
+                if (c[u] >= 0) {
+                    lds_col[wave][rank[u]] = c[u];
+                    out.sorted[(int64_t)n * T + rank[u]] = c[u];
+                    out.place[(int64_t)n * T + rank[u]] = (uint16_t)(64 * u + lane);
+                }
+                there += __popcll(__ballot(c[u] >= 0));
+            }
+            __builtin_amdgcn_wave_barrier();      // the wave's own LDS, in order
+            const int slabs = (V + out.slab - 1) / out.slab;
+            for (int s = lane; s <= slabs + 1; s += 64) {     // (a tile may end a slab later)
+                // entries before column s·slab
+                const int64_t edge = (int64_t)s * out.slab;
+                int lo = 0, hi = there;
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (lds_col[wave][mid] < edge) lo = mid + 1;
+                    else hi = mid;
+                }
+                out.first[(int64_t)n * out.ldfirst + s] = (uint16_t)lo;
+            }
         }
-        // l is 0 without a target, NaN where an entry is
-        if (lane == 0) mass[n] = l == 0.f ? 0.f : 1.f;
+        if (out.mass) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                p[u] = sum[u];
+                if (again[u]) c[u] = -1;
+            }
+            // l is 0 without a target, NaN where an entry is
+            if (lane == 0) out.mass[n] = l == 0.f ? 0.f : 1.f;
+        }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int j = 64 * u + lane;
         if (j < T) {
-            col[(int64_t)n * T + j] = c[u];
-            p_out[(int64_t)n * T + j] = p[u];
-            if (logp_out) logp_out[(int64_t)n * T + j] = lp[u];
+            out.col[(int64_t)n * T + j] = c[u];
+            out.p[(int64_t)n * T + j] = p[u];
+            if (out.logp) out.logp[(int64_t)n * T + j] = lp[u];
         }
     }
 }
@@ -134,10 +166,10 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict_
 // STAT_COLS columns of one token: 256 threads of 4 x 4 columns each, kept in
 // registers between the maximum and the sum.
 __global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S, int64_t lds, int c0, int cols,
-                                                    float inv_t, LossTargets t, float2* __restrict__ part, int ldpart,
-                                                    int part0, float* __restrict__ picked, int64_t ldpk) {
+                                                    float inv_t, LossTargets t, float2* __restrict__ part, int N,
+                                                    int part0, int n0, float* __restrict__ picked, int64_t ldpk) {
     __shared__ float red[8];
-    const int n = blockIdx.y;
+    const int n = n0 + blockIdx.y;
     const int b0 = blockIdx.x * STAT_COLS;
     const int left = cols - b0 < STAT_COLS ? cols - b0 : STAT_COLS;
     const float* row = S + (int64_t)n * lds + b0;
@@ -172,7 +204,7 @@ __global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S,
     __syncthreads();
     if (threadIdx.x == 0) {
         l = (red[4] + red[5]) + (red[6] + red[7]);
-        part[(int64_t)n * ldpart + part0 + blockIdx.x] = make_float2(l == 0.f ? -INFINITY : base, l);
+        part[(int64_t)(part0 + blockIdx.x) * N + n] = make_float2(l == 0.f ? -INFINITY : base, l);
     }
     for (int j = threadIdx.x; j < t.T; j += 256) {
         const int64_t c = (t.labels ? t.labels[n] : (int64_t)t.col[(int64_t)n * t.T + j]) - c0 - b0;
@@ -180,42 +212,59 @@ __global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S,
     }
 }
 
-// One wave per token.
-__global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ part, int ldpart, int nparts, int N,
-                                                     int V, float tt, LossTargets t, float* __restrict__ picked,
+// 16 tokens: 16 threads each join every 16th part of a token, in order; the wave's
+// lanes then take a token's entries.
+__global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ part, int nparts, int N, int V,
+                                                     float tt, LossTargets t, float* __restrict__ picked,
                                                      int64_t ldpk, float* __restrict__ loss, float* __restrict__ lse) {
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (n >= N) return;
+    __shared__ float red_m[16][17], red_l[16][17], lse_of[16];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    const int n = blockIdx.x * 16 + x;
     float m = -INFINITY, l = 0.f;
-    for (int i = lane; i < nparts; i += 64) {
-        const float2 q = part[(int64_t)n * ldpart + i];
-        const float to = fmaxf(m, q.x);
-        l = rescale(l, m, to) + rescale(q.y, q.x, to);
-        m = to;
+    if (n < N)
+        for (int i = y; i < nparts; i += 16) {
+            const float2 q = part[(int64_t)i * N + n];
+            const float to = fmaxf(m, q.x);
+            l = rescale(l, m, to) + rescale(q.y, q.x, to);
+            m = to;
+        }
+    red_m[y][x] = m;
+    red_l[y][x] = l;
+    __syncthreads();
+    if (y == 0) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, red_m[i][x]);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += rescale(red_l[i][x], red_m[i][x], top);
+        const float ls = top + logf(sum);
+        lse_of[x] = ls;
+        if (n < N) {
+            lse[n] = ls;
+            if (t.labels) {
+                const int64_t c = t.labels[n];
+                loss[n] = c >= V ? nan_f() : (c >= 0 ? ls - picked[(int64_t)n * ldpk] : 0.f);
+            }
+        }
     }
-    const float top = wave_max(m);
-    l = wave_sum(rescale(l, m, top));
-    const float ls = top + logf(l);
-    float v = 0.f;
-    if (t.labels) {
-        const int64_t c = t.labels[n];
-        if (c >= V) v = nan_f();
-        else if (c >= 0) v = ls - picked[(int64_t)n * ldpk];
-    } else {
+    if (t.labels) return;
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int k = wave; k < 16 && (int)blockIdx.x * 16 + k < N; k += 4) {
+        const int64_t row = (int64_t)blockIdx.x * 16 + k;
+        const float ls = lse_of[k];
+        float v = 0.f;
         for (int j = lane; j < t.T; j += 64) {
-            const int64_t at = (int64_t)n * t.T + j;
+            const int64_t at = row * t.T + j;
             if (t.col[at] < 0) {
-                picked[(int64_t)n * ldpk + j] = 0.f;
+                picked[row * ldpk + j] = 0.f;
             } else if (t.p[at] != 0.f) {
-                v += t.p[at] * ((t.logp[at] + ls) - picked[(int64_t)n * ldpk + j]);
+                v += t.p[at] * ((t.logp[at] + ls) - picked[row * ldpk + j]);
             }
         }
         v = wave_sum(v) * tt;
-    }
-    if (lane == 0) {
-        loss[n] = v;
-        lse[n] = ls;
+        if (lane == 0) loss[row] = v;
     }
 }
 
@@ -250,86 +299,117 @@ __global__ __launch_bounds__(1024) void coef_kernel(const float* __restrict__ dl
 __device__ __forceinline__ uint16_t to_elem(float v, uint16_t) { return (uint16_t)bf16_rne(v); }
 __device__ __forceinline__ float to_elem(float v, float) { return v; }
 
-// 64 x 64 of G, its transpose through LDS.
+__device__ __forceinline__ float from_elem(uint16_t v) { return bf16_to_f32(v); }
+__device__ __forceinline__ float from_elem(float v) { return v; }
+__device__ __forceinline__ uint16_t zero_of(uint16_t) { return 0; }
+__device__ __forceinline__ float zero_of(float) { return 0.f; }
+
+// 64 x 64 of G, its transpose through LDS.  Term 1 is what term 0's rounding left.
 template <typename E>
 __global__ __launch_bounds__(256) void grad_kernel(const float* __restrict__ S, int64_t lds, int N, int c0, int cols,
                                                    float inv_t, const float* __restrict__ lse,
                                                    const float* __restrict__ r, const int64_t* __restrict__ labels,
-                                                   E* __restrict__ G, int64_t ldg, E* __restrict__ GT, int64_t ldgt) {
+                                                   GradOut out) {
     __shared__ E tile[64][64 + 4 / sizeof(E)];
     const int n0 = blockIdx.y * 64, b0 = blockIdx.x * 64;
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4;    // 4 columns, 16 rows a pass
+    float g[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int n = n0 + i * 16 + y, c = b0 + 4 * x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[i][e] = 0.f;
         if (n >= N || c >= cols) continue;
         const float rn = r[n];
-        f32x4_t s = *reinterpret_cast<const f32x4_t*>(S + (int64_t)n * lds + c);
+        const f32x4_t s = *reinterpret_cast<const f32x4_t*>(S + (int64_t)n * lds + c);
         const float ls = lse[n];
         const int64_t at = labels ? labels[n] - c0 - c : -1;
-        E g[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float v = exp_f(s[e] * inv_t - ls);
             if (at == e) v -= 1.f;
             // a token without a target: 0 whatever its logits are
-            g[e] = to_elem(rn == 0.f ? 0.f : rn * v, E());
-            tile[i * 16 + y][4 * x + e] = g[e];
+            g[i][e] = rn == 0.f ? 0.f : rn * v;
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < cols) G[(int64_t)n * ldg + c + e] = g[e];
     }
-    __syncthreads();
+    for (int term = 0; term < out.terms; ++term) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = b0 + i * 16 + y, n = n0 + 4 * x;
-        if (c >= cols) continue;
+        for (int i = 0; i < 4; ++i) {
+            const int n = n0 + i * 16 + y, c = b0 + 4 * x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < N) GT[(int64_t)c * ldgt + n + e] = tile[4 * x + e][i * 16 + y];
+            for (int e = 0; e < 4; ++e) {
+                const E q = to_elem(g[i][e], E());
+                g[i][e] -= from_elem(q);
+                tile[i * 16 + y][4 * x + e] = q;
+                if (out.G && n < N && c + e < cols) ((E*)out.G)[((int64_t)term * N + n) * out.ldg + c + e] = q;
+            }
+        }
+        if (!out.GT) continue;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = b0 + i * 16 + y, n = n0 + 4 * x;
+            if (c >= cols) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < out.ldx) ((E*)out.GT)[c * out.ldgt + term * out.ldx + n + e] = tile[4 * x + e][i * 16 + y];
+        }
+        __syncthreads();
     }
 }
 
 template <typename E>
 __global__ __launch_bounds__(256) void fix_kernel(LossTargets t, const float* __restrict__ picked, int64_t ldpk,
-                                                  const float* __restrict__ lse, const float* __restrict__ r,
-                                                  int64_t total, int c0, int cols, E* __restrict__ G, int64_t ldg,
-                                                  E* __restrict__ GT, int64_t ldgt) {
+                                                  const float* __restrict__ lse, const float* __restrict__ r, int N,
+                                                  int c0, int cols, GradOut out) {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= total) return;
+    if (at >= (int64_t)N * t.T) return;
     const int c = t.col[at] - c0;
     if (t.col[at] < 0 || c < 0 || c >= cols) return;
     const int n = (int)(at / t.T), j = (int)(at - (int64_t)n * t.T);
     const float rn = r[n];
     if (rn == 0.f) return;
-    const E g = to_elem(rn * (exp_f(picked[(int64_t)n * ldpk + j] - lse[n]) - t.p[at]), E());
-    G[(int64_t)n * ldg + c] = g;
-    GT[(int64_t)c * ldgt + n] = g;
+    float g = rn * (exp_f(picked[(int64_t)n * ldpk + j] - lse[n]) - t.p[at]);
+    for (int term = 0; term < out.terms; ++term) {
+        const E q = to_elem(g, E());
+        g -= from_elem(q);
+        if (out.G) ((E*)out.G)[((int64_t)term * N + n) * out.ldg + c] = q;
+        if (out.GT) ((E*)out.GT)[c * out.ldgt + term * out.ldx + n] = q;
+    }
 }
 
-__device__ __forceinline__ uint16_t zero_of(uint16_t) { return 0; }
-__device__ __forceinline__ float zero_of(float) { return 0.f; }
-
+// 64 x 64 through LDS, 16 bytes a load and a store.
 template <typename E>
-__global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict__ X, int64_t ldx,
+__global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict__ X, int64_t ldx_,
                                                              const float* __restrict__ r, int N, int K,
-                                                             E* __restrict__ dst, int64_t ldd) {
+                                                             E* __restrict__ dst, int64_t ldd, int64_t ldx, int terms) {
+    constexpr int W = 16 / sizeof(E), PER = 64 / W;          // elements of a piece, pieces of 64
     __shared__ E tile[64][64 + 4 / sizeof(E)];
     const int n0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int n = n0 + i * 4 + y, k = k0 + x;
-        E v = zero_of(E());
-        if (n < N && k < K && r[n] != 0.f) v = X[(int64_t)n * ldx + k];
-        tile[i * 4 + y][x] = v;
+#pragma unroll
+    for (int q = threadIdx.x; q < 64 * PER; q += 256) {
+        const int n = n0 + q / PER, k = k0 + q % PER * W;
+        struct { E v[W]; } x;
+        u32x4_t raw = {0u, 0u, 0u, 0u};
+        // rows of X are padded to 16 bytes
+        if (n < N && k < K && r[n] != 0.f) raw = *reinterpret_cast<const u32x4_t*>(X + (int64_t)n * ldx_ + k);
+        __builtin_memcpy(&x, &raw, 16);
+#pragma unroll
+        for (int e = 0; e < W; ++e) tile[q / PER][q % PER * W + e] = x.v[e];
     }
     __syncthreads();
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int k = k0 + i * 4 + y, n = n0 + x;
-        if (k < K && n < N) dst[(int64_t)k * ldd + n] = tile[x][i * 4 + y];
+#pragma unroll
+    for (int q = threadIdx.x; q < 64 * PER; q += 256) {
+        const int k = k0 + q / PER, n = n0 + q % PER * W;
+        // ldx is a multiple of 8: a piece that starts before it ends there
+        if (k >= K || n >= ldx) continue;
+        struct { E v[W]; } x;
+#pragma unroll
+        for (int e = 0; e < W; ++e) x.v[e] = tile[q % PER * W + e][q / PER];
+        u32x4_t raw;
+        __builtin_memcpy(&raw, &x, 16);
+        for (int term = 0; term < terms; ++term)
+            *reinterpret_cast<u32x4_t*>(dst + (int64_t)k * ldd + term * ldx + n) = raw;
     }
 }
 
@@ -339,18 +419,39 @@ __global__ __launch_bounds__(256) void add_f32_kernel(f32x4_t* __restrict__ acc,
         acc[i] += src[i];
 }
 
+// 8 columns a thread
 template <typename E>
-__global__ __launch_bounds__(256) void scale_out_kernel(const float* __restrict__ src, int64_t lds,
-                                                        const float* __restrict__ scale, E* __restrict__ out,
-                                                        int64_t ldo, int64_t R, int64_t C) {
+__global__ __launch_bounds__(256) void sum_out_kernel(const float* __restrict__ src, int64_t lds, int slabs,
+                                                      int64_t stride, const float* __restrict__ scale,
+                                                      E* __restrict__ out, int64_t ldo, int64_t R, int64_t C) {
     const float a = scale[0];
-    const int64_t quads = (C + 3) / 4, total = R * quads;
+    const int64_t pieces = (C + 7) / 8, total = R * pieces;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / quads, c = (i - row * quads) * 4;
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(src + row * lds + c);
+        const int64_t row = i / pieces, c = (i - row * pieces) * 8;
+        // rows of src are padded to a multiple of 8 columns
+        const float* p = src + row * lds + c;
+        f32x4_t lo = *reinterpret_cast<const f32x4_t*>(p), hi = *reinterpret_cast<const f32x4_t*>(p + 4);
+        for (int s = 1; s < slabs; ++s) {
+            lo += *reinterpret_cast<const f32x4_t*>(p + s * stride);
+            hi += *reinterpret_cast<const f32x4_t*>(p + s * stride + 4);
+        }
+        struct { E v[8]; } q;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < C) out[row * ldo + c + e] = to_elem(a * v[e], E());
+        for (int e = 0; e < 4; ++e) {
+            q.v[e] = to_elem(a * lo[e], E());
+            q.v[4 + e] = to_elem(a * hi[e], E());
+        }
+        E* o = out + row * ldo + c;
+        if (c + 8 <= C) {
+            u32x4_t raw[sizeof(E) / 2];
+            __builtin_memcpy(raw, &q, 8 * sizeof(E));
+#pragma unroll
+            for (int e = 0; e < (int)sizeof(E) / 2; ++e) reinterpret_cast<u32x4_t*>(o)[e] = raw[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < C) o[e] = q.v[e];
+        }
     }
 }
 
@@ -369,11 +470,10 @@ unsigned blocks_of(int64_t items, int64_t most = 16384) {
 }  // namespace
 
 hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits, int64_t ldl, int N, int T, int V,
-                          float inv_t, bool merge, int* col, float* p, float* logp, float* mass, hipStream_t stream) {
+                          float inv_t, const TeacherOut& out, hipStream_t stream) {
     const dim3 grid((N + 3) / 4), block(256);
-#define TEACHER(U)                                                                                                  \
-    hipLaunchKernelGGL(teacher_kernel<U>, grid, block, 0, stream, index, ldi, logits, ldl, N, T, V, inv_t, merge ? 1 : 0, \
-                       col, p, logp, mass)
+#define TEACHER(U) \
+    hipLaunchKernelGGL(teacher_kernel<U>, grid, block, 0, stream, index, ldi, logits, ldl, N, T, V, inv_t, out)
     if (T <= 64) TEACHER(1);
     else if (T <= 128) TEACHER(2);
     else if (T <= 256) TEACHER(4);
@@ -384,24 +484,21 @@ hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits
 }
 
 hipError_t launch_loss_stats(const float* S, int64_t lds, int N, int c0, int cols, float inv_t,
-                             const LossTargets& t, float2* part, int ldpart, int part0, float* picked, int64_t ldpk,
+                             const LossTargets& t, float2* part, int part0, float* picked, int64_t ldpk,
                              hipStream_t stream) {
     // a launch has at most 65535 workgroups in y
     const int chunks = (cols + STAT_COLS - 1) / STAT_COLS;
     for (int n0 = 0; n0 < N; n0 += 65535) {
         const int rows = N - n0 < 65535 ? N - n0 : 65535;
-        LossTargets u = t;
-        if (u.labels) u.labels += n0;
-        if (u.col) u.col += (int64_t)n0 * t.T;
-        hipLaunchKernelGGL(stats_kernel, dim3(chunks, rows), dim3(256), 0, stream, S + (int64_t)n0 * lds, lds, c0, cols,
-                           inv_t, u, part + (int64_t)n0 * ldpart, ldpart, part0, picked + (int64_t)n0 * ldpk, ldpk);
+        hipLaunchKernelGGL(stats_kernel, dim3(chunks, rows), dim3(256), 0, stream, S, lds, c0, cols, inv_t, t, part, N,
+                           part0, n0, picked, ldpk);
     }
     return hipGetLastError();
 }
 
-hipError_t launch_loss_finish(const float2* part, int ldpart, int nparts, int N, int V, float temperature, const LossTargets& t,
+hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, float temperature, const LossTargets& t,
                               float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream) {
-    hipLaunchKernelGGL(finish_kernel, dim3((N + 3) / 4), dim3(256), 0, stream, part, ldpart, nparts, N, V,
+    hipLaunchKernelGGL(finish_kernel, dim3((N + 15) / 16), dim3(256), 0, stream, part, nparts, N, V,
                        temperature * temperature, t, picked, ldpk, loss, lse);
     return hipGetLastError();
 }
@@ -412,51 +509,42 @@ hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const flo
     return hipGetLastError();
 }
 
+// N < 2^22 tokens: at most 65536 workgroups of 64 rows in y
+static_assert((1 << 22) / 64 <= 65536, "launch limit");
+
 hipError_t launch_loss_grad(const float* S, int64_t lds, int N, int c0, int cols, float inv_t, const float* lse,
-                            const float* r, const int64_t* labels, void* G, int64_t ldg, void* GT, int64_t ldgt,
-                            bool f32, hipStream_t stream) {
-    const int tc = (cols + 63) / 64;
-    for (int n0 = 0; n0 < N; n0 += 65535 * 64) {
-        const int rows = N - n0 < 65535 * 64 ? N - n0 : 65535 * 64;
-        const dim3 grid(tc, (rows + 63) / 64), block(256);
-        if (f32)
-            hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S + (int64_t)n0 * lds, lds, rows, c0, cols,
-                               inv_t, lse + n0, r + n0, labels ? labels + n0 : nullptr, (float*)G + (int64_t)n0 * ldg,
-                               ldg, (float*)GT + n0, ldgt);
-        else
-            hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S + (int64_t)n0 * lds, lds, rows, c0,
-                               cols, inv_t, lse + n0, r + n0, labels ? labels + n0 : nullptr,
-                               (uint16_t*)G + (int64_t)n0 * ldg, ldg, (uint16_t*)GT + n0, ldgt);
-    }
+                            const float* r, const int64_t* labels, const GradOut& out, hipStream_t stream) {
+    const dim3 grid((cols + 63) / 64, (N + 63) / 64), block(256);
+    if (out.f32)
+        hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S, lds, N, c0, cols, inv_t, lse, r, labels, out);
+    else
+        hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S, lds, N, c0, cols, inv_t, lse, r, labels,
+                           out);
     return hipGetLastError();
 }
 
 hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ldpk, const float* lse, const float* r,
-                           int N, int c0, int cols, void* G, int64_t ldg, void* GT, int64_t ldgt, bool f32,
-                           hipStream_t stream) {
-    const int64_t total = (int64_t)N * t.T;
-    const dim3 grid((unsigned)((total + 255) / 256)), block(256);
-    if (f32)
-        hipLaunchKernelGGL(fix_kernel<float>, grid, block, 0, stream, t, picked, ldpk, lse, r, total, c0, cols,
-                           (float*)G, ldg, (float*)GT, ldgt);
+                           int N, int c0, int cols, const GradOut& out, hipStream_t stream) {
+    const dim3 grid((unsigned)(((int64_t)N * t.T + 255) / 256)), block(256);
+    if (out.f32)
+        hipLaunchKernelGGL(fix_kernel<float>, grid, block, 0, stream, t, picked, ldpk, lse, r, N, c0, cols, out);
     else
-        hipLaunchKernelGGL(fix_kernel<uint16_t>, grid, block, 0, stream, t, picked, ldpk, lse, r, total, c0, cols,
-                           (uint16_t*)G, ldg, (uint16_t*)GT, ldgt);
+        hipLaunchKernelGGL(fix_kernel<uint16_t>, grid, block, 0, stream, t, picked, ldpk, lse, r, N, c0, cols, out);
     return hipGetLastError();
 }
 
-hipError_t launch_transpose_live(const void* X, int64_t ldx, const float* r, int N, int K, void* dst, int64_t ldd,
-                                 bool f32, hipStream_t stream) {
+hipError_t launch_transpose_live(const void* X, int64_t ldx_, const float* r, int N, int K, void* dst, int64_t ldd,
+                                 int64_t ldx, int terms, bool f32, hipStream_t stream) {
     // at most 65535 workgroups in y
     for (int k0 = 0; k0 < K; k0 += 65535 * 64) {
         const int k = K - k0 < 65535 * 64 ? K - k0 : 65535 * 64;
         const dim3 grid((N + 63) / 64, (k + 63) / 64), block(256);
         if (f32)
-            hipLaunchKernelGGL(transpose_live_kernel<float>, grid, block, 0, stream, (const float*)X + k0, ldx, r, N, k,
-                               (float*)dst + (int64_t)k0 * ldd, ldd);
+            hipLaunchKernelGGL(transpose_live_kernel<float>, grid, block, 0, stream, (const float*)X + k0, ldx_, r, N,
+                               k, (float*)dst + (int64_t)k0 * ldd, ldd, ldx, terms);
         else
-            hipLaunchKernelGGL(transpose_live_kernel<uint16_t>, grid, block, 0, stream, (const uint16_t*)X + k0, ldx, r,
-                               N, k, (uint16_t*)dst + (int64_t)k0 * ldd, ldd);
+            hipLaunchKernelGGL(transpose_live_kernel<uint16_t>, grid, block, 0, stream, (const uint16_t*)X + k0, ldx_,
+                               r, N, k, (uint16_t*)dst + (int64_t)k0 * ldd, ldd, ldx, terms);
     }
     return hipGetLastError();
 }
@@ -467,14 +555,15 @@ hipError_t launch_add_f32(float* acc, const float* src, int64_t elems, hipStream
     return hipGetLastError();
 }
 
-hipError_t launch_scale_out(const float* src, int64_t lds, const float* scale, void* out, int64_t ldo, int64_t R,
-                            int64_t C, bool f32, hipStream_t stream) {
-    const dim3 grid(blocks_of(R * ((C + 3) / 4))), block(256);
+hipError_t launch_sum_out(const float* src, int64_t lds, int slabs, int64_t stride, const float* scale, void* out,
+                          int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream) {
+    const dim3 grid(blocks_of(R * ((C + 7) / 8))), block(256);
     if (f32)
-        hipLaunchKernelGGL(scale_out_kernel<float>, grid, block, 0, stream, src, lds, scale, (float*)out, ldo, R, C);
+        hipLaunchKernelGGL(sum_out_kernel<float>, grid, block, 0, stream, src, lds, slabs, stride, scale, (float*)out,
+                           ldo, R, C);
     else
-        hipLaunchKernelGGL(scale_out_kernel<uint16_t>, grid, block, 0, stream, src, lds, scale, (uint16_t*)out, ldo, R,
-                           C);
+        hipLaunchKernelGGL(sum_out_kernel<uint16_t>, grid, block, 0, stream, src, lds, slabs, stride, scale,
+                           (uint16_t*)out, ldo, R, C);
     return hipGetLastError();
 }
 

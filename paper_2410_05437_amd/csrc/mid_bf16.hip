@@ -275,7 +275,7 @@ hipError_t launch_cfg_mid(const GemmArgs& g, bool upper, hipStream_t stream) {
                        S > 1 || upper || g.c_f32 ? g.partial : nullptr, ldp, stride, (steps + S - 1) / S,
                        upper ? 1 : 0);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || S == 1 || upper) return e;
+    if (e != hipSuccess || S == 1 || upper || g.c_f32) return e;
     return launch_splitk_reduce(g.partial, S, stride, ldp, g.C, g.ldc, g.R, g.Cc, g.c_pairs ? 2 : 1, stream);
 }
 
@@ -341,7 +341,7 @@ static hipError_t launch_config(const GemmArgs& g, bool upper, hipStream_t strea
 
 hipError_t launch_mid_tn_bf16(const GemmArgs& g, hipStream_t stream) {
     if (!mid_supported(g.lda, g.ldb) || g.a_pairs) return hipErrorInvalidValue;
-    if (g.c_f32 && (g.splits > 1 || g.C != g.partial || g.ldc != splitk_ld(g.Cc))) return hipErrorInvalidValue;
+    if (g.c_f32 && (g.C != g.partial || g.ldc != splitk_ld(g.Cc))) return hipErrorInvalidValue;
     return launch_config(g, false, stream);
 }
 

@@ -21,45 +21,70 @@ struct LossTargets {
 // Columns of S that one workgroup of launch_loss_stats reduces.
 constexpr int STAT_COLS = 4096;
 
-// The teacher's distributions: col[n][j] its entry (-1: empty), p[n][j], logp[n][j].
-// merge: an entry that occurs again is added to its first place, whose other places
-// become empty, and mass[n] is 1, or 0 for a token without a target.
+// The teacher's distributions: col[n][j] its entry (-1: empty), p[n][j] and, if
+// wanted, logp[n][j].
+struct TeacherOut {
+    int* col = nullptr;
+    float* p = nullptr;
+    float* logp = nullptr;
+    // wanted for the backward pass: an entry that occurs again is added to its first
+    // place, whose other places become empty, and mass[n] is 1, or 0 for a token
+    // without a target
+    float* mass = nullptr;
+    // wanted for LossEpi: the entries in the order of their columns, their places, and
+    // how many lie before each slab of `slab` columns, up to the second past the last
+    // (rows ldfirst apart)
+    int* sorted = nullptr;
+    uint16_t* place = nullptr;
+    uint16_t* first = nullptr;
+    int64_t ldfirst = 0;
+    int slab = 1;
+};
 hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits, int64_t ldl, int N, int T, int V,
-                          float inv_t, bool merge, int* col, float* p, float* logp, float* mass, hipStream_t stream);
+                          float inv_t, const TeacherOut& out, hipStream_t stream);
 
 // Columns [c0, c0 + cols) of the logits, S [N][lds] float32: the largest s / t and Σ
-// exp(s / t - it) of every STAT_COLS of them at part[n][part0 ...], and s / t of the
-// targets among them at picked[n][j].
+// exp(s / t - it) of every STAT_COLS of them at part[k][n] (k from part0 on), and s / t
+// of the targets among them at picked[n][j].
 hipError_t launch_loss_stats(const float* S, int64_t lds, int N, int c0, int cols, float inv_t,
-                             const LossTargets& t, float2* part, int ldpart, int part0, float* picked, int64_t ldpk,
+                             const LossTargets& t, float2* part, int part0, float* picked, int64_t ldpk,
                              hipStream_t stream);
-// loss and lse from nparts parts of each token (rows ldpart apart); picked of empty
-// places.
-hipError_t launch_loss_finish(const float2* part, int ldpart, int nparts, int N, int V, float temperature, const LossTargets& t,
+// loss and lse from the nparts parts of each token; picked of empty places.
+hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, float temperature, const LossTargets& t,
                               float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream);
 
 // r[n] = coef[n] / c and scale[0] = c, with coef the factor of token n's row of G (0
 // without a target) and c the largest of their magnitudes.
 hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
                             float* r, float* scale, hipStream_t stream);
-// G [N][ldg] and its transpose GT [cols][ldgt] of columns [c0, c0 + cols) from S
-// (type f32 or bfloat16); labels may be NULL (their entries are launch_loss_fix's).
+// A piece of G, N rows and `cols` columns, and its transpose (either NULL: not wanted).
+// terms 2: bfloat16 entries as a sum of two, the second N rows on in G and ldx columns
+// on in GT (whose columns [N, ldx) are then zeros).
+struct GradOut {
+    void* G = nullptr;
+    int64_t ldg = 0;
+    void* GT = nullptr;
+    int64_t ldgt = 0;
+    int64_t ldx = 0;
+    int terms = 1;
+    bool f32 = false;
+};
+// G of columns [c0, c0 + cols) from S; labels may be NULL (their entries are
+// launch_loss_fix's).
 hipError_t launch_loss_grad(const float* S, int64_t lds, int N, int c0, int cols, float inv_t, const float* lse,
-                            const float* r, const int64_t* labels, void* G, int64_t ldg, void* GT, int64_t ldgt,
-                            bool f32, hipStream_t stream);
+                            const float* r, const int64_t* labels, const GradOut& out, hipStream_t stream);
 // The teacher's entries among these columns, from their logits `picked`.
 hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ldpk, const float* lse, const float* r,
-                           int N, int c0, int cols, void* G, int64_t ldg, void* GT, int64_t ldgt, bool f32,
-                           hipStream_t stream);
-// dst[k][n] = X[n][k], 0 where r[n] is 0.
-hipError_t launch_transpose_live(const void* X, int64_t ldx, const float* r, int N, int K, void* dst, int64_t ldd,
-                                 bool f32, hipStream_t stream);
+                           int N, int c0, int cols, const GradOut& out, hipStream_t stream);
+// dst[k][n] = X[n][k], 0 where r[n] is 0 and in the columns [N, ldx); terms 2: once
+// more ldx columns on.
+hipError_t launch_transpose_live(const void* X, int64_t ldx_, const float* r, int N, int K, void* dst, int64_t ldd,
+                                 int64_t ldx, int terms, bool f32, hipStream_t stream);
 // acc += src (rows of ld elements, a multiple of 4)
 hipError_t launch_add_f32(float* acc, const float* src, int64_t elems, hipStream_t stream);
-// out[r][c] = scale[0]·src[r][c]
-hipError_t launch_scale_out(const float* src, int64_t lds, const float* scale, void* out, int64_t ldo, int64_t R,
-                            int64_t C, bool f32, hipStream_t stream);
-
+// out[r][c] = scale[0]·Σ of `slabs` of src, `stride` apart, in their order
+hipError_t launch_sum_out(const float* src, int64_t lds, int slabs, int64_t stride, const float* scale, void* out,
+                          int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream);
 // zeros in the columns [0, C) of R rows
 hipError_t launch_zero(void* out, int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream);
 

@@ -3,6 +3,7 @@
 #include "espace_train.h"
 
 #include <cmath>
+#include <cstdio>
 #include <algorithm>
 
 #include "api.hpp"
@@ -15,69 +16,121 @@ namespace {
 
 using espace::LossTargets;
 
-constexpr int64_t kMaxTokens = (int64_t)1 << 22;
+constexpr int64_t kMaxTokens = (int64_t)1 << 21;
 
 int64_t ld8(int64_t c) { return (c + 7) / 8 * 8; }
 
-// Columns of a piece of the logits: about 2^25 of them (128 MB of float32, half the
-// Infinity Cache), in pieces of equal width, a multiple of 256.
-int64_t piece_cols(int64_t N, int64_t V) {
-    const int64_t most = std::max<int64_t>(((int64_t)1 << 25) / std::max<int64_t>(N, 1) / 256, 1) * 256;
+// Columns of a piece of the vocabulary, a multiple of 256: the most that keep N·columns
+// within `elems`, in whole rounds of 256 x 256 tiles on all CUs where those fit, else in
+// pieces of equal width.
+int64_t piece_cols(int64_t N, int64_t V, int64_t elems) {
+    const int64_t most = std::max<int64_t>(elems / N / 256, 1) * 256;
+    if (V <= most) return V;
+    const int64_t tr = (N + 255) / 256;
+    int64_t round = 256;                           // tile columns of whole rounds
+    for (int64_t t = tr; t % 2 == 0 && round > 1; t /= 2) round /= 2;
+    if (round * 256 <= most) return most / (round * 256) * (round * 256);
     const int64_t pieces = (V + most - 1) / most;
-    return std::min(((V + pieces - 1) / pieces + 255) / 256 * 256, V);
+    return ((V + pieces - 1) / pieces + 255) / 256 * 256;
 }
 
+// Pieces that are kept as float32 logits: 128 MB, half the Infinity Cache.  Those of G
+// where the logits stay in registers (bfloat16; G and its transpose): the same.
+constexpr int64_t kLogits = (int64_t)1 << 25, kGrads = (int64_t)1 << 25;
+// Where the epilogues cannot take a call's leading dimensions: narrow pieces, which fit
+// any layout.
+constexpr int64_t kNarrow = 256;
+// Tokens up to which a bfloat16 entry of G is kept as the sum of two: the entries of a
+// few tokens carry their roundings alone (65 tokens of 8 teacher's entries: dX and dW
+// 2.4e-3 off, 1.7e-3 with two, the rounding of the results), and the products of so few
+// are bound by reading W.
+constexpr int64_t kTwoTerms = 128;
+// Depth ranges of dX's product, left to the pass that rounds it, and the floats of
+// their sums.
+constexpr int64_t kRanges = 16, kRangeFloats = (int64_t)1 << 24;
+
 struct Layout {
-    size_t S, part, picked, col, p, logp, total;             // forward
-    size_t mass, r, scale, XT, G, GT, WT, acc, slab, out;    // backward
-    int64_t P, lds, nparts;
-    int64_t ldn, ldp, ldk;
+    size_t S, part, picked, col, p, logp, sorted, place, first;    // forward (S, col, p: both)
+    size_t mass, r, scale, XT, G, GT, WT, acc, out, total;         // backward
+    int tile;                    // >= 0: the logits' epilogues on this tile
+    int slab;                    // columns of their slabs
+    int64_t P;                   // columns of a piece
+    int terms;
+    int tile_x, tile_w;          // >= 0: dX, dW from the gradients' epilogue
+    int ranges;                  // of dX's product otherwise
+    int64_t ldn, ldp, ldk, ldfirst;
 };
 
 Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, espace_dtype dt) {
     Layout b{};
     const size_t es = elem_size(dt);
+    const bool bf16 = dt == ESPACE_BF16;
     size_t o = 0;
     auto take = [&](size_t bytes) {
         const size_t at = o;
         o = align_ws(o + bytes);
         return at;
     };
-    b.P = piece_cols(N, V);
-    b.lds = espace::splitk_ld((int)b.P);
-    const int64_t pieces = (V + b.P - 1) / b.P;
-    b.nparts = pieces * ((b.P + espace::STAT_COLS - 1) / espace::STAT_COLS);
-    b.S = take((size_t)N * b.lds * 4);
+    b.terms = bf16 && N <= kTwoTerms ? 2 : 1;
+    b.P = backward ? piece_cols(N, V, kGrads) : V;
+    b.tile = bf16 && b.terms == 1 ? f32_tile(N, b.P, K, ld8(K), ld8(K)) : -1;
+    if (b.tile < 0) b.P = piece_cols(N, V, kLogits);
+    b.slab = espace::loss_slab(b.tile);
+    b.S = take((size_t)N * espace::splitk_ld((int)(b.tile < 0 ? b.P : std::min(V, kNarrow))) * 4);
     if (T > 0) {
         b.col = take((size_t)N * T * 4);
         b.p = take((size_t)N * T * 4);
     }
     if (!backward) {
-        b.part = take((size_t)N * b.nparts * 8);
-        if (T > 0) b.logp = take((size_t)N * T * 4);
-        else b.picked = take((size_t)N * 4);
+        const int64_t pieces = (V + b.P - 1) / b.P, stats = (b.P + espace::STAT_COLS - 1) / espace::STAT_COLS;
+        const int64_t slabs = (V + b.slab - 1) / b.slab;
+        b.part = take((size_t)N * (b.tile < 0 ? pieces * stats : std::max(slabs + 1, (V + kNarrow - 1) / kNarrow)) * 8);
+        if (T > 0) {
+            b.logp = take((size_t)N * T * 4);
+            if (b.tile >= 0) {
+                b.ldfirst = slabs + 2;
+                b.sorted = take((size_t)N * T * 4);
+                b.place = take((size_t)N * T * 2);
+                b.first = take((size_t)N * b.ldfirst * 2);
+            }
+        } else {
+            b.picked = take((size_t)N * 4);
+        }
         b.total = o;
         return b;
     }
+    const int64_t pieces = (V + b.P - 1) / b.P;
     b.ldn = ld8(N);
     b.ldp = ld8(b.P);
     b.ldk = espace::splitk_ld((int)K);
     if (T > 0) b.mass = take((size_t)N * 4);
     b.r = take((size_t)N * 4);
     b.scale = take(4);
-    b.XT = take((size_t)K * b.ldn * es);
-    b.G = take((size_t)N * b.ldp * es);
-    b.GT = take((size_t)b.P * b.ldn * es);
+    b.XT = take((size_t)K * b.ldn * b.terms * es);
+    b.G = take((size_t)N * b.terms * b.ldp * es);
+    b.GT = take((size_t)b.P * b.ldn * b.terms * es);
     b.WT = take((size_t)K * b.ldp * es);
-    b.acc = take((size_t)N * b.ldk * 4);
-    if (pieces > 1) b.slab = take((size_t)N * b.ldk * 4);
-    b.out = take((size_t)b.P * b.ldk * 4);
+    b.tile_x = b.tile_w = -1;
+    if (b.tile >= 0) {
+        // each gradient's sums from its own epilogue, dX's unless its tiles leave most
+        // CUs without one and ranges of the depth can be summed later
+        b.tile_x = f32_tile(N, K, b.P, b.ldp, b.ldp);
+        b.tile_w = f32_tile(b.P, K, N, b.ldn, b.ldn);
+        const int64_t tiles = (N + 255) / 256 * ((K + 255) / 256);
+        if (pieces <= 4 && 2 * tiles < device_cus()) b.tile_x = -1;
+    }
+    // without the epilogue: the ranges of up to 4 pieces, or two float32 sums
+    b.ranges = (int)std::max<int64_t>(1, std::min(kRanges, kRangeFloats / (N * b.terms * b.ldk)));
+    const int64_t sums = b.tile_x >= 0 ? (pieces > 1 ? 1 : 0) : (pieces <= 4 && bf16 ? b.ranges * pieces : std::min<int64_t>(pieces, 2));
+    // (a call whose leading dimensions take it to narrow pieces has two)
+    b.acc = take((size_t)N * b.terms * b.ldk * 4 * std::max<int64_t>(sums, b.tile >= 0 ? 2 : 1));
+    b.out = take((size_t)(b.tile_w >= 0 ? std::min(V, kNarrow) : b.P) * b.ldk * 4);
     b.total = o;
     return b;
 }
 
 espace_status check_sizes(int64_t N, int64_t K, int64_t V) {
-    if (N < 0 || N >= kMaxTokens) return fail(ESPACE_ERR_SHAPE, "need 0 <= N < 2^22 tokens (N=%lld)", (long long)N);
+    if (N < 0 || N >= kMaxTokens) return fail(ESPACE_ERR_SHAPE, "need 0 <= N < 2^21 tokens (N=%lld)", (long long)N);
     if (K < 1 || K > kMaxDim || V < 1 || V > kMaxDim)
         return fail(ESPACE_ERR_SHAPE, "need 1 <= K, V <= 2^30 (K=%lld, V=%lld)", (long long)K, (long long)V);
     return ESPACE_OK;
@@ -136,6 +189,8 @@ espace_status check_temperature(int64_t T, float t) {
         if (_e != hipSuccess) return fail(ESPACE_ERR_HIP, what ": %s", hipGetErrorString(_e)); \
     } while (0)
 
+const int64_t kLim = (int64_t)1 << 31;
+
 // columns [c0, c0 + cols) of the logits, float32
 espace_status logits_piece(const void* X, int64_t ldx, const void* W, int64_t ldw, float* S, int64_t N, int64_t K,
                            int64_t c0, int64_t cols, espace_dtype dt, hipStream_t stream) {
@@ -143,23 +198,61 @@ espace_status logits_piece(const void* X, int64_t ldx, const void* W, int64_t ld
                       espace::splitk_ld((int)cols), N, cols, K, dt, stream);
 }
 
+void log_plan(const Layout& b, bool backward, bool fused, int64_t N, int64_t K, int64_t V, int64_t T, int64_t P) {
+    if (!plan_log()) return;
+    std::fprintf(stderr,
+                 "espace loss plan N=%lld K=%lld V=%lld T=%lld: backward=%d fused=%d tile=%d columns=%lld terms=%d "
+                 "tile_x=%d tile_w=%d ranges=%d\n",
+                 (long long)N, (long long)K, (long long)V, (long long)T, backward, fused, b.tile, (long long)P, b.terms,
+                 b.tile_x, b.tile_w, b.ranges);
+}
+
 espace_status loss_forward(const void* X, int64_t ldx, const void* W, int64_t ldw, LossTargets t, float* loss,
                            float* lse, float* picked, int64_t ldpk, int64_t N, int64_t K, int64_t V,
                            float temperature, espace_dtype dt, const Layout& b, char* ws, hipStream_t stream) {
     float* S = (float*)(ws + b.S);
     float2* part = (float2*)(ws + b.part);
-    int part0 = 0;
-    for (int64_t c0 = 0; c0 < V; c0 += b.P) {
-        const int64_t cols = std::min(b.P, V - c0);
-        ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, stream));
-        ESPACE_LAUNCH("loss statistics",
-                      espace::launch_loss_stats(S, espace::splitk_ld((int)cols), (int)N, (int)c0, (int)cols,
-                                                1.f / temperature, t, part, (int)b.nparts, part0, picked, ldpk, stream));
-        part0 += (int)((cols + espace::STAT_COLS - 1) / espace::STAT_COLS);
+    const float inv_t = 1.f / temperature;
+    int parts = 0;
+    // the epilogue's launches: rows of W below 2^31 elements, in whole slabs of either width
+    const int64_t step = 768;
+    const bool fused = b.tile >= 0 && N * ldx < kLim && std::min(V, step) * ldw < kLim;
+    log_plan(b, false, fused, N, K, V, t.labels ? 0 : t.T, fused ? V : (b.tile >= 0 ? std::min(V, kNarrow) : b.P));
+    if (fused) {
+        const int64_t most = V * ldw < kLim ? V : (kLim - 1) / ldw / step * step;
+        for (int64_t c0 = 0; c0 < V; c0 += most) {
+            const int64_t cols = std::min(most, V - c0);
+            espace::LossEpi e;
+            e.inv_t = inv_t;
+            e.col0 = (int)c0;
+            e.labels = t.labels;
+            e.part = part + (size_t)(c0 / b.slab) * N;
+            e.picked = picked;
+            e.ldpk = ldpk;
+            if (!t.labels) {
+                e.col = (int*)(ws + b.sorted);
+                e.place = (uint16_t*)(ws + b.place);
+                e.first = (uint16_t*)(ws + b.first);
+                e.ldfirst = b.ldfirst;
+                e.T = t.T;
+            }
+            ESPACE_TRY(run_tn_loss(X, ldx, (const uint16_t*)W + c0 * ldw, ldw, nullptr, 0, N, cols, K, b.tile,
+                                   espace::LOSS_STATS, e, stream));
+        }
+        parts = (int)((V + b.slab - 1) / b.slab);
+    } else {
+        const int64_t P = b.tile >= 0 ? std::min(V, kNarrow) : b.P;
+        for (int64_t c0 = 0; c0 < V; c0 += P) {
+            const int64_t cols = std::min(P, V - c0);
+            ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, stream));
+            ESPACE_LAUNCH("loss statistics",
+                          espace::launch_loss_stats(S, espace::splitk_ld((int)cols), (int)N, (int)c0, (int)cols, inv_t,
+                                                    t, part, parts, picked, ldpk, stream));
+            parts += (int)((cols + espace::STAT_COLS - 1) / espace::STAT_COLS);
+        }
     }
-    // the last piece may have had fewer parts than the others
-    ESPACE_LAUNCH("loss", espace::launch_loss_finish(part, (int)b.nparts, part0, (int)N, (int)V, temperature, t, picked,
-                                                     ldpk, loss, lse, stream));
+    ESPACE_LAUNCH("loss", espace::launch_loss_finish(part, parts, (int)N, (int)V, temperature, t, picked, ldpk, loss,
+                                                     lse, stream));
     return ESPACE_OK;
 }
 
@@ -173,35 +266,92 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     float* r = (float*)(ws + b.r);
     float* scale = (float*)(ws + b.scale);
     float* acc = (float*)(ws + b.acc);
-    float* slab = (float*)(ws + b.slab);
     float* out = (float*)(ws + b.out);
     void *XT = ws + b.XT, *G = ws + b.G, *GT = ws + b.GT, *WT = ws + b.WT;
+    const float inv_t = 1.f / temperature;
+    const bool fused = b.tile >= 0 && N * ldx < kLim && b.P * ldw < kLim;
+    const int tile_x = fused ? b.tile_x : -1, tile_w = fused ? b.tile_w : -1;
+    const int64_t P = b.tile >= 0 && !fused ? std::min(V, kNarrow) : b.P;
+    const int64_t pieces = (V + P - 1) / P;
+    const int64_t rows = N * b.terms, slab = rows * b.ldk;      // of dX's sums
+    const bool many = tile_x < 0 && pieces <= 4 && !f32 && !(b.tile >= 0 && !fused);
+    const int ranges = many ? b.ranges : 1;
+    const int64_t ldgt = b.ldn * b.terms;
+    int sums = 0;                                               // slabs in acc
+    log_plan(b, true, fused, N, K, V, t.labels ? 0 : t.T, P);
     ESPACE_LAUNCH("loss coefficients", espace::launch_loss_coef(dloss, t.labels, mass, temperature, (int)N, (int)V, r,
                                                                 scale, stream));
-    if (dW) ESPACE_LAUNCH("transpose", espace::launch_transpose_live(X, ldx, r, (int)N, (int)K, XT, b.ldn, f32, stream));
-    for (int64_t c0 = 0; c0 < V; c0 += b.P) {
-        const int64_t cols = std::min(b.P, V - c0);
-        const int64_t lds = espace::splitk_ld((int)cols);
+    if (dW)
+        ESPACE_LAUNCH("transpose", espace::launch_transpose_live(X, ldx, r, (int)N, (int)K, XT, ldgt, b.ldn, b.terms,
+                                                                 f32, stream));
+    for (int64_t c0 = 0; c0 < V; c0 += P) {
+        const int64_t cols = std::min(P, V - c0);
         const char* Wp = (const char*)W + (size_t)c0 * ldw * es;
-        ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, stream));
-        ESPACE_LAUNCH("logits' gradient", espace::launch_loss_grad(S, lds, (int)N, (int)c0, (int)cols,
-                                                                   1.f / temperature, lse, r, t.labels, G, b.ldp, GT,
-                                                                   b.ldn, f32, stream));
+        const bool last = c0 + cols == V;
+        espace::GradOut go;
+        go.G = dX || fused ? G : nullptr;
+        go.ldg = b.ldp;
+        go.GT = dW && !fused ? GT : nullptr;
+        go.ldgt = ldgt;
+        go.ldx = b.ldn;
+        go.terms = b.terms;
+        go.f32 = f32;
+        if (fused) {
+            espace::LossEpi e;
+            e.inv_t = inv_t;
+            e.col0 = (int)c0;
+            e.labels = t.labels;
+            e.lse = lse;
+            e.r = r;
+            ESPACE_TRY(run_tn_loss(X, ldx, Wp, ldw, G, b.ldp, N, cols, K, b.tile, espace::LOSS_GRAD, e, stream));
+        } else {
+            ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, stream));
+            ESPACE_LAUNCH("logits' gradient",
+                          espace::launch_loss_grad(S, espace::splitk_ld((int)cols), (int)N, (int)c0, (int)cols, inv_t,
+                                                   lse, r, t.labels, go, stream));
+        }
         if (!t.labels)
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
-                                                                       (int)cols, G, b.ldp, GT, b.ldn, f32, stream));
+                                                                       (int)cols, go, stream));
+        if (dW && fused)
+            ESPACE_LAUNCH("transpose", espace::launch_transpose(G, b.ldp, (int)N, (int)cols, GT, b.ldn, f32, stream));
         if (dX) {
             ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, b.ldp, f32, stream));
-            ESPACE_TRY(run_tn_f32(G, b.ldp, WT, b.ldp, c0 ? slab : acc, b.ldk, N, K, cols, dt, stream));
-            if (c0) ESPACE_LAUNCH("sum", espace::launch_add_f32(acc, slab, N * b.ldk, stream));
+            if (tile_x >= 0) {
+                espace::LossEpi e;
+                e.acc = acc;
+                e.ldacc = b.ldk;
+                e.scale = scale;
+                e.add = c0 > 0;
+                e.last = last;
+                ESPACE_TRY(run_tn_loss(G, b.ldp, WT, b.ldp, dX, lddx, N, K, cols, tile_x, espace::LOSS_GRAD_OUT, e,
+                                       stream));
+            } else {
+                int made = 1;
+                ESPACE_TRY(run_tn_f32(G, b.ldp, WT, b.ldp, acc + sums * slab, b.ldk, rows, K, cols, dt, stream, ranges,
+                                      &made));
+                if (many || !sums) sums += made;
+                else ESPACE_LAUNCH("sum", espace::launch_add_f32(acc, acc + slab, slab, stream));
+            }
         }
         if (dW) {
-            ESPACE_TRY(run_tn_f32(GT, b.ldn, XT, b.ldn, out, b.ldk, cols, K, N, dt, stream));
-            ESPACE_LAUNCH("gradient", espace::launch_scale_out(out, b.ldk, scale, (char*)dW + (size_t)c0 * lddw * es,
-                                                               lddw, cols, K, f32, stream));
+            void* o = (char*)dW + (size_t)c0 * lddw * es;
+            if (tile_w >= 0) {
+                espace::LossEpi e;
+                e.scale = scale;
+                e.last = 1;
+                ESPACE_TRY(run_tn_loss(GT, ldgt, XT, ldgt, o, lddw, cols, K, N, tile_w, espace::LOSS_GRAD_OUT, e,
+                                       stream));
+            } else {
+                ESPACE_TRY(run_tn_f32(GT, ldgt, XT, ldgt, out, b.ldk, cols, K, b.terms > 1 ? b.ldn + N : N, dt, stream));
+                ESPACE_LAUNCH("gradient", espace::launch_sum_out(out, b.ldk, 1, 0, scale, o, lddw, cols, K, f32, stream));
+            }
         }
     }
-    if (dX) ESPACE_LAUNCH("gradient", espace::launch_scale_out(acc, b.ldk, scale, dX, lddx, N, K, f32, stream));
+    if (dX && tile_x < 0)
+        // a second term's rows are a slab of their own
+        ESPACE_LAUNCH("gradient", espace::launch_sum_out(acc, b.ldk, sums * b.terms, N * b.ldk, scale, dX, lddx, N, K,
+                                                         f32, stream));
     return ESPACE_OK;
 }
 
@@ -234,9 +384,19 @@ espace_status forward(const void* X, int64_t ldx, const void* W, int64_t ldw, co
         t.p = (float*)(ws + b.p);
         t.logp = (float*)(ws + b.logp);
         t.T = (int)T;
+        espace::TeacherOut to;
+        to.col = (int*)(ws + b.col);
+        to.p = (float*)(ws + b.p);
+        to.logp = (float*)(ws + b.logp);
+        if (b.tile >= 0) {
+            to.sorted = (int*)(ws + b.sorted);
+            to.place = (uint16_t*)(ws + b.place);
+            to.first = (uint16_t*)(ws + b.first);
+            to.ldfirst = b.ldfirst;
+            to.slab = b.slab;
+        }
         ESPACE_LAUNCH("teacher", espace::launch_teacher(index, ldi, logits, ldl, (int)N, (int)T, (int)V,
-                                                        1.f / temperature, false, (int*)(ws + b.col),
-                                                        (float*)(ws + b.p), (float*)(ws + b.logp), nullptr, stream));
+                                                        1.f / temperature, to, stream));
     } else {
         picked = (float*)(ws + b.picked);
         ldpk = 1;
@@ -286,9 +446,12 @@ espace_status backward(const float* dloss, const void* X, int64_t ldx, const voi
         t.col = (int*)(ws + b.col);
         t.p = (float*)(ws + b.p);
         t.T = (int)T;
+        espace::TeacherOut to;
+        to.col = (int*)(ws + b.col);
+        to.p = (float*)(ws + b.p);
+        to.mass = mass;
         ESPACE_LAUNCH("teacher", espace::launch_teacher(index, ldi, logits, ldl, (int)N, (int)T, (int)V,
-                                                        1.f / temperature, true, (int*)(ws + b.col),
-                                                        (float*)(ws + b.p), nullptr, mass, stream));
+                                                        1.f / temperature, to, stream));
     }
     return loss_backward(X, ldx, W, ldw, t, dloss, mass, lse, picked, ldpk, dX, lddx, dW, lddw, N, K, V, temperature,
                          dt, b, ws, stream);

@@ -177,7 +177,9 @@ __device__ __forceinline__ void v3_substep(f32x4_t (&acc)[V3_NB][C::NBJ], const 
         }
 }
 
-enum { V3_BF16 = 0, V3_F32 = 1, V3_PAIR = 2 };
+enum { V3_BF16 = 0, V3_F32 = 1, V3_PAIR = 2,
+       // the products of a loss on the logits of a head (LossEpi)
+       V3_STATS = 3, V3_GRAD = 4, V3_GRAD_OUT = 5 };
 
 // byte offsets of this lane's 16-byte chunk of each wave-load (depth offset
 // excluded) for the tile at (row0, col0): row 16q + lane/4 of the A|B tile,

@@ -63,7 +63,7 @@ def test_valid_calls_reach_the_device():
 def test_loss_refusals():
     for call in (_ce, _ceb, _kd, _kdb):
         assert call(X=NULL) == 1 and call(W=NULL) == 1 and call(lse=NULL) == 1
-        assert call(N=-1) == 2 and call(N=1 << 22) == 2 and call(K=0) == 2 and call(V=0) == 2 and call(V=1 << 31) == 2
+        assert call(N=-1) == 2 and call(N=1 << 21) == 2 and call(K=0) == 2 and call(V=0) == 2 and call(V=1 << 31) == 2
         assert call(ldx=56) == 2 and call(ldw=56) == 2 and call(ldx=68) == 3
         assert call(X=off(P(1), 8)) == 3 and call(lse=off(P(5), 2)) == 3
         assert call(dt=2) == 4
@@ -98,7 +98,7 @@ def test_loss_workspace_sizes():
     ws = L.espace_linear_loss_workspace_bytes
     for b in (0, 1):
         assert ws(b, 0, 64, 100, 0, 1) == 0
-        assert ws(b, -1, 64, 100, 0, 1) == BIG and ws(b, 1 << 22, 64, 100, 0, 1) == BIG
+        assert ws(b, -1, 64, 100, 0, 1) == BIG and ws(b, 1 << 21, 64, 100, 0, 1) == BIG
         assert ws(b, 8, 0, 100, 0, 1) == BIG and ws(b, 8, 64, 0, 0, 1) == BIG
         assert ws(b, 8, 64, 100, -1, 1) == BIG and ws(b, 8, 64, 100, 1025, 1) == BIG and ws(b, 8, 64, 100, 4, 5) == BIG
         assert 0 < ws(b, 8, 64, 100, 0, 0) < ws(b, 8, 64, 100, 4, 0)
@@ -117,11 +117,11 @@ def _embb(tokens=P(1), dX=P(2), lddx=64, dE=P(3), ldde=64, N=8, K=64, V=100, acc
 
 def test_embedding_refusals():
     assert _emb(tokens=NULL) == 1 and _emb(e=NULL) == 1 and _emb(X=NULL) == 1
-    assert _emb(N=-1) == 2 and _emb(N=1 << 22) == 2 and _emb(K=0) == 2 and _emb(V=0) == 2
+    assert _emb(N=-1) == 2 and _emb(N=1 << 21) == 2 and _emb(K=0) == 2 and _emb(V=0) == 2
     assert _emb(lde=56) == 2 and _emb(ldx=60) == 2 and _emb(ldx=68) == 3 and _emb(tokens=off(P(1), 4)) == 3
     assert _emb(dt=9) == 4 and _emb(X=off(P(2), 128)) == 5 and _emb(X=P(1)) == 5
     assert _embb(tokens=NULL) == 1 and _embb(dX=NULL) == 1 and _embb(dE=NULL) == 1
-    assert _embb(N=1 << 22) == 2 and _embb(K=0) == 2 and _embb(V=0) == 2 and _embb(ldde=56) == 2 and _embb(lddx=65) == 3
+    assert _embb(N=1 << 21) == 2 and _embb(K=0) == 2 and _embb(V=0) == 2 and _embb(ldde=56) == 2 and _embb(lddx=65) == 3
     assert _embb(dt=-1) == 4 and _embb(dE=off(P(2), 128)) == 5 and _embb(ws=P(2)) == 5 and _embb(ws=P(3)) == 5
     assert _embb(ws=NULL) == 6 and _embb(wsb=64) == 6 and _embb(ws=off(P(4), 8)) == 3
     assert L.espace_embedding_workspace_bytes(-1, 64, 100) == BIG

@@ -86,7 +86,7 @@ class Loss:
         # sums over V or N; the output rounded
         dq = q * (self.ds + self.dlse + 4 * U * ((self.s - self.lse).abs() + 1)) + dtarget + 2 * U * (q + target)
         h = HALF_STEP[self.dtype]
-        step = (h * h * 2 if two_terms else h) if self.dtype == torch.bfloat16 else 0.0
+        step = (h * h if two_terms else h) if self.dtype == torch.bfloat16 else 0.0
         dG = coef.abs() * dq * (1 + 2 * h) + (step + 4 * U) * G.abs() + 1e-36
         x = torch.where(live[:, None], self.x, 0.0)
         N, V = G.shape
