@@ -20,7 +20,7 @@
  * workspaces, statuses, streams; the same call on the same operands gives the same
  * bits again), with these additions: int64 and float32 arrays need their natural
  * alignment alone, a leading dimension of index, logits and picked any value >= T.
- * Limits: 1 <= V, 1 <= K, N < 2^21 (more tokens: several calls).
+ * Limits: 1 <= V <= 2^30, 1 <= K <= 2^21, N < 2^21 (more tokens: several calls).
  *
  * Tokens without a target are part of the call and have no loss: it is 0, their row
  * of dX is 0, and they add nothing to dW, whatever their rows of X and their dloss

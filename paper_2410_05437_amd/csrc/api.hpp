@@ -47,15 +47,24 @@ espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, voi
 
 // The same with C in float32 whatever the operands' type, ldc = splitk_ld(Cc) and C
 // the library's own scratch: columns up to ldc may be written.  Needs no partial
-// sums.  ranges > 1 (bfloat16): the sums of up to so many depth ranges, *made of them,
-// R·ldc apart in C, not combined.
+// sums.  ranges > 1: the sums of up to so many depth ranges, *made of them, R·ldc apart
+// in C, not combined.
 espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
                          int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream, int ranges = 1,
                          int* made = nullptr);
-// bfloat16: the tile (256 x 256 or 256 x 192) that run_tn_f32 takes in one range, or -1
-// where another kernel is priced below these or takes the sizes.
-int f32_tile(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb);
-// A product of a loss (LossEpi) on such a tile.
+// Its plan for bfloat16: the cheapest of 256 x 256 and 256 x 192 tiles, priced as the
+// other tiled products, and the small tiles; one or two rows may take the streaming
+// kernel, matrices past the kernels' offsets one with 64-bit ones.
+struct F32Plan {
+    enum Kind { WIDE, GEMV, MID, TILED } kind = WIDE;
+    int tile = -1;            // of kind TILED; the small tiles' configuration of kind MID
+    int ranges = 1;
+};
+F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges);
+// C = scale[0]·A·Bᵀ rounded to bfloat16, on the small tiles of such a plan in one range.
+espace_status run_tn_scaled_mid(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
+                                int64_t R, int64_t Cc, int64_t D, int config, const float* scale, hipStream_t stream);
+// A product of a loss (LossEpi) on a tile of kind TILED.
 espace_status run_tn_loss(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R,
                           int64_t Cc, int64_t D, int tile, LossMode mode, const LossEpi& epi, hipStream_t stream);
 

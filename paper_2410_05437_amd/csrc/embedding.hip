@@ -10,11 +10,13 @@
 //    entry and by which of its 16 waves' shares of the tokens), then placing them.
 //    No workgroup waits for another.  A token's place among equal ones in its wave's
 //    64 is found from ballots of the entry's bits.
-//  * reduce: a workgroup sums RUN_BLOCK sorted places, and writes the rows of the
-//    entries that begin and end there.  An entry that goes on in the next block (a
-//    frequent token, half the batch's padding) leaves a float32 partial row per
-//    block; further workgroups write the zeros of the entries without a token.
+//  * reduce: blocks of sorted places; the entries that begin and end in a block are
+//    written.  An entry that goes on in the next block (a frequent token, half the
+//    batch's padding) leaves a float32 partial row per block; further workgroups write
+//    the zeros of the entries without a token.
 //  * join: the partial rows of each such entry, added in order.
+#include <algorithm>
+
 #include "common.hpp"
 #include "train.hpp"
 
@@ -78,10 +80,10 @@ __global__ __launch_bounds__(256) void embedding_kernel(const int64_t* __restric
 
 constexpr int SORT_WAVES = 16;
 constexpr int SORT_BINS = 1024;           // entries per workgroup, at most
-constexpr int RUN_BLOCK = 32;             // sorted places per workgroup
+constexpr int SORT_AHEAD = 8;             // groups of 64 tokens whose loads are in flight
 
 __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int64_t* __restrict__ tokens, int N, int V,
-                                                                      int bins, int* __restrict__ order,
+                                                                      int bins, int bits, int* __restrict__ order,
                                                                       int* __restrict__ start) {
     __shared__ int count[SORT_WAVES][SORT_BINS];
     __shared__ int sums[SORT_WAVES];
@@ -89,17 +91,30 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int6
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lo = blockIdx.x * bins;
     const int nb = V - lo < bins ? V - lo : bins;
-    for (int i = threadIdx.x; i < SORT_WAVES * SORT_BINS; i += SORT_WAVES * 64) (&count[0][0])[i] = 0;
+    for (int w = 0; w < SORT_WAVES; ++w)
+        for (int i = threadIdx.x; i < nb; i += SORT_WAVES * 64) count[w][i] = 0;
     __syncthreads();
     // this wave's share of the tokens, whole groups of 64
     const int groups = (N + 63) / 64, per = (groups + SORT_WAVES - 1) / SORT_WAVES;
     const int g0 = wave * per, g1 = g0 + per < groups ? g0 + per : groups;
+    // entries of SORT_AHEAD groups, relative to lo; -1 for a token outside the table or
+    // this wave's share
+    int64_t t[SORT_AHEAD];
+    auto load = [&](int g) {
+#pragma unroll
+        for (int u = 0; u < SORT_AHEAD; ++u) {
+            const int n = (g + u) * 64 + lane;
+            t[u] = g + u < g1 && n < N ? tokens[n] : -1;
+        }
+    };
     int below = 0;
-    for (int g = g0; g < g1; ++g) {
-        const int n = g * 64 + lane;
-        const int64_t t = n < N ? tokens[n] : -1;
-        if (t >= 0 && t < lo) ++below;
-        if (t >= lo && t < lo + nb) atomicAdd(&count[wave][(int)t - lo], 1);
+    for (int g = g0; g < g1; g += SORT_AHEAD) {
+        load(g);
+#pragma unroll
+        for (int u = 0; u < SORT_AHEAD; ++u) {
+            if (t[u] >= 0 && t[u] < lo) ++below;
+            if (t[u] >= lo && t[u] < lo + nb) atomicAdd(&count[wave][(int)t[u] - lo], 1);
+        }
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) below += __shfl_xor(below, m);
@@ -134,84 +149,107 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int6
         }
     }
     __syncthreads();
-    for (int g = g0; g < g1; ++g) {
-        const int n = g * 64 + lane;
-        const int64_t t = n < N ? tokens[n] : -1;
-        const bool in = t >= lo && t < lo + nb;
-        unsigned long long same = __ballot(in);
-        if (same == 0) continue;
-        const int bin = in ? (int)t - lo : 0;
-        // lanes with the same entry
+    for (int g = g0; g < g1; g += SORT_AHEAD) {
+        load(g);
 #pragma unroll
-        for (int bit = 0; bit < 10; ++bit) {
-            const unsigned long long on = __ballot((bin >> bit) & 1);
-            same &= ((bin >> bit) & 1) ? on : ~on;
-        }
-        if (in) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            const int place = count[wave][bin] + rank;
-            order[place] = n;
-            // the last of the equal lanes moves the place on; the wave's lanes have
-            // all read it (one wave, in order)
+        for (int u = 0; u < SORT_AHEAD; ++u) {
+            const bool in = t[u] >= lo && t[u] < lo + nb;
+            unsigned long long same = __ballot(in);
+            if (same == 0) continue;
+            const int bin = in ? (int)t[u] - lo : 0;
+            // lanes with the same entry
+            for (int bit = 0; bit < bits; ++bit) {
+                const unsigned long long on = __ballot((bin >> bit) & 1);
+                same &= ((bin >> bit) & 1) ? on : ~on;
+            }
+            if (in) {
+                const int rank = __popcll(same & ((1ull << lane) - 1));
+                const int place = count[wave][bin] + rank;
+                order[place] = (g + u) * 64 + lane;
+                // the last of the equal lanes moves the place on; the wave's lanes
+                // have all read it (one wave, in order)
+                __builtin_amdgcn_wave_barrier();
+                if ((same >> lane) == 1ull) count[wave][bin] = place + 1;
+            }
             __builtin_amdgcn_wave_barrier();
-            if ((same >> lane) == 1ull) count[wave][bin] = place + 1;
         }
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
-// Sum of the runs in places [p0, p1) for the 256 x W columns of blockIdx.y.
+// How the rows' columns lie on a workgroup's threads: `per_row` threads (a power of
+// two) of 16 bytes each, workgroup y taking the per_row · W columns from y on; so
+// narrow rows leave room for several at a time.
+constexpr int RUN_MOST = 32;              // sorted places of a block of runs, at most
+constexpr int ROWS_AHEAD = 8;             // rows whose loads are in flight
+
+// Sums of the runs in blocks of `places` sorted places, a block for every `per_row`
+// threads.  A run that goes on in the next block, or comes from the one before, leaves
+// its sum in the block's part 1, or 0 (one that does both: 0).  Workgroups from
+// run_groups on write the zeros of the entries without a token, RUN_MOST each.
 template <typename E>
 __global__ __launch_bounds__(256) void reduce_runs_kernel(const int64_t* __restrict__ tokens,
                                                           const E* __restrict__ dX, int64_t lddx, E* __restrict__ dE,
                                                           int64_t ldde, int64_t K, int V, float scale, int accumulate,
                                                           const int* __restrict__ order, const int* __restrict__ start,
-                                                          float* __restrict__ part, int64_t ldpart, int run_blocks) {
+                                                          float* __restrict__ part, int64_t ldpart, int run_groups,
+                                                          int places, int per_row) {
     constexpr int W = Piece<E>::W;
-    const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * W;
-    if ((int)blockIdx.x >= run_blocks) {
-        // zeros for the entries without a token, RUN_BLOCK entries a workgroup
-        const int v0 = ((int)blockIdx.x - run_blocks) * RUN_BLOCK;
-        const int v1 = v0 + RUN_BLOCK < V ? v0 + RUN_BLOCK : V;
+    const int group = threadIdx.x / per_row, groups = 256 / per_row;
+    const int64_t c = ((int64_t)blockIdx.y * per_row + threadIdx.x % per_row) * W;
+    if ((int)blockIdx.x >= run_groups) {
+        const int v0 = ((int)blockIdx.x - run_groups) * RUN_MOST;
+        const int lane = threadIdx.x & 63;
+        // one bit an entry, in every wave
+        const int mine = v0 + (lane < RUN_MOST ? lane : RUN_MOST - 1);
+        const bool none = lane < RUN_MOST && mine < V && start[mine] == start[mine + 1];
+        const unsigned long long empty = __ballot(none);
         Piece<E> z;
 #pragma unroll
         for (int e = 0; e < W; ++e) z.v[e] = to_elem(0.f, E());
-        for (int v = v0; v < v1; ++v)
-            if (start[v] == start[v + 1] && c < K) store_piece(dE + (int64_t)v * ldde, c, K, z);
+        if (c < K)
+            for (int k = group; k < RUN_MOST; k += groups)
+                if ((empty >> k) & 1) store_piece(dE + (int64_t)(v0 + k) * ldde, c, K, z);
         return;
     }
-    __shared__ int row[RUN_BLOCK], entry[RUN_BLOCK];
+    // rows of the workgroup's places, and the entries of those and their neighbours
+    // (-1 before the first and past the last)
+    __shared__ int row[256 / 8 * RUN_MOST], entry[256 / 8 * RUN_MOST + 2];
     const int total = start[V];
-    const int p0 = blockIdx.x * RUN_BLOCK;
-    if (p0 >= total) return;
-    const int np = total - p0 < RUN_BLOCK ? total - p0 : RUN_BLOCK;
-    if (threadIdx.x < (unsigned)np) {
-        row[threadIdx.x] = order[p0 + threadIdx.x];
-        entry[threadIdx.x] = (int)tokens[row[threadIdx.x]];
+    const int all = groups * places, first = blockIdx.x * all;
+    for (int i = threadIdx.x; i < all + 2; i += 256) {
+        const int p = first + i - 1;
+        int n = -1, v = -1;
+        if (p >= 0 && p < total) {
+            n = order[p];
+            v = (int)tokens[n];
+        }
+        entry[i] = v;
+        if (i >= 1 && i <= all) row[i - 1] = n;
     }
     __syncthreads();
-    if (c >= K) return;
+    const int q0 = group * places;
+    const int np = min(places, total - first - q0);
+    if (np <= 0 || c >= K) return;
+    const int block = blockIdx.x * groups + group;
     float sum[W];
 #pragma unroll
     for (int e = 0; e < W; ++e) sum[e] = 0.f;
-    constexpr int AHEAD = 8;
-    for (int q = 0; q < np; q += AHEAD) {
-        Piece<E> x[AHEAD];
+    bool from_before = entry[q0] == entry[q0 + 1];
+    for (int q = 0; q < np; q += ROWS_AHEAD) {
+        Piece<E> x[ROWS_AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int at = q + u < np ? q + u : np - 1;
-            x[u] = load_piece(dX + (int64_t)row[at] * lddx + c);
-        }
+        for (int u = 0; u < ROWS_AHEAD; ++u)
+            x[u] = load_piece(dX + (int64_t)row[q0 + min(q + u, np - 1)] * lddx + c);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
+        for (int u = 0; u < ROWS_AHEAD; ++u) {
             if (q + u >= np) break;
 #pragma unroll
             for (int e = 0; e < W; ++e) sum[e] += to_f32(x[u].v[e]);
-            const int v = entry[q + u];
-            if (q + u + 1 < np && entry[q + u + 1] == v) continue;
+            const int v = entry[q0 + q + u + 1];
+            const bool goes_on = entry[q0 + q + u + 2] == v;
+            if (goes_on && q + u + 1 < np) continue;
             // the run's last place in this block
-            const int s = start[v], t = start[v + 1];
-            if (s >= p0 && t <= p0 + np) {
+            if (!from_before && !goes_on) {
                 E* out = dE + (int64_t)v * ldde;
                 Piece<E> o;
                 if (accumulate) o = load_piece(out + c);
@@ -220,45 +258,70 @@ __global__ __launch_bounds__(256) void reduce_runs_kernel(const int64_t* __restr
                     o.v[e] = to_elem(accumulate ? to_f32(o.v[e]) + scale * sum[e] : scale * sum[e], E());
                 store_piece(out, c, K, o);
             } else {
-                // slot 0: a run that came from the block before, slot 1: one that starts here
-                float* o = part + ((int64_t)blockIdx.x * 2 + (s < p0 ? 0 : 1)) * ldpart + c;
+                float* o = part + ((int64_t)block * 2 + (from_before ? 0 : 1)) * ldpart + c;
 #pragma unroll
                 for (int e = 0; e < W; e += 4)
                     *reinterpret_cast<f32x4_t*>(o + e) = f32x4_t{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
             }
+            from_before = false;
 #pragma unroll
             for (int e = 0; e < W; ++e) sum[e] = 0.f;
         }
     }
 }
 
-// The entry whose run starts in block blockIdx.x and goes on in the next ones.
+// The entry whose run starts in block blockIdx.x and goes on in the next ones: each
+// per_row threads add a contiguous share of its parts, in order; the shares are added
+// in order through LDS.
+constexpr int JOIN_THREADS = 1024;
+
 template <typename E>
-__global__ __launch_bounds__(256) void join_runs_kernel(const int64_t* __restrict__ tokens, E* __restrict__ dE,
-                                                        int64_t ldde, int64_t K, int V, float scale, int accumulate,
-                                                        const int* __restrict__ order, const int* __restrict__ start,
-                                                        const float* __restrict__ part, int64_t ldpart) {
+__global__ __launch_bounds__(JOIN_THREADS) void join_runs_kernel(const int64_t* __restrict__ tokens,
+                                                                 E* __restrict__ dE, int64_t ldde, int64_t K, int V,
+                                                                 float scale, int accumulate,
+                                                                 const int* __restrict__ order,
+                                                                 const int* __restrict__ start,
+                                                                 const float* __restrict__ part, int64_t ldpart,
+                                                                 int places, int per_row) {
     constexpr int W = Piece<E>::W;
-    const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * W;
-    const int total = start[V];
-    const int p0 = blockIdx.x * RUN_BLOCK, p1 = p0 + RUN_BLOCK;
-    if (p1 >= total || c >= K) return;
+    __shared__ float shares[JOIN_THREADS * W];
+    const int p1 = ((int)blockIdx.x + 1) * places;
+    if (p1 >= start[V]) return;
     const int v = (int)tokens[order[p1 - 1]];
     const int s = start[v], t = start[v + 1];
-    if (s < p0 || t <= p1) return;
+    if (s < p1 - places || t <= p1) return;
+    const int group = threadIdx.x / per_row, groups = JOIN_THREADS / per_row;
+    const int64_t c = ((int64_t)blockIdx.y * per_row + threadIdx.x % per_row) * W;
+    // part 1 of this block, part 0 of the next ones
+    const int parts = (t - 1) / places - (int)blockIdx.x + 1;
+    const int share = (parts + groups - 1) / groups;
+    const int k0 = group * share, k1 = min(k0 + share, parts);
     float sum[W];
-    auto add = [&](int64_t slot, bool first) {
-        const float* p = part + slot * ldpart + c;
 #pragma unroll
-        for (int e = 0; e < W; e += 4) {
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + e);
+    for (int e = 0; e < W; ++e) sum[e] = 0.f;
+    if (c < K)
+        for (int k = k0; k < k1; k += ROWS_AHEAD) {
+            f32x4_t x[ROWS_AHEAD][W / 4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[e + i] = first ? x[i] : sum[e + i] + x[i];
+            for (int u = 0; u < ROWS_AHEAD; ++u) {
+                const int q = min(k + u, k1 - 1);
+                const float* p = part + (((int64_t)blockIdx.x + q) * 2 + (q == 0 ? 1 : 0)) * ldpart + c;
+#pragma unroll
+                for (int e = 0; e < W / 4; ++e) x[u][e] = reinterpret_cast<const f32x4_t*>(p)[e];
+            }
+#pragma unroll
+            for (int u = 0; u < ROWS_AHEAD; ++u)
+                if (k + u < k1)
+#pragma unroll
+                    for (int e = 0; e < W; ++e) sum[e] += x[u][e / 4][e % 4];
         }
-    };
-    const int last = (t - 1) / RUN_BLOCK;
-    add((int64_t)blockIdx.x * 2 + 1, true);
-    for (int k = blockIdx.x + 1; k <= last; ++k) add((int64_t)k * 2, false);
+#pragma unroll
+    for (int e = 0; e < W; ++e) shares[threadIdx.x * W + e] = sum[e];
+    __syncthreads();
+    if (group != 0 || c >= K) return;
+    for (int g = 1; g < groups && g * share < parts; ++g)
+#pragma unroll
+        for (int e = 0; e < W; ++e) sum[e] += shares[(g * per_row + threadIdx.x) * W + e];
     E* out = dE + (int64_t)v * ldde;
     Piece<E> o;
     if (accumulate) o = load_piece(out + c);
@@ -266,6 +329,21 @@ __global__ __launch_bounds__(256) void join_runs_kernel(const int64_t* __restric
     for (int e = 0; e < W; ++e)
         o.v[e] = to_elem(accumulate ? to_f32(o.v[e]) + scale * sum[e] : scale * sum[e], E());
     store_piece(out, c, K, o);
+}
+
+// Sorted places of a block: the most that leave 512 workgroups, two a CU.
+int run_places(int64_t N, int64_t K, int per_row, int W) {
+    const int64_t chunks = (K + (int64_t)per_row * W - 1) / ((int64_t)per_row * W);
+    int places = RUN_MOST;
+    while (places > 8 && (N + places - 1) / places * per_row / 256 * chunks < 512) places /= 2;
+    return places;
+}
+
+// Threads of a row: the power of two from 8 to 256 that holds K in 16-byte pieces.
+int row_threads(int64_t K, int W) {
+    int t = 8;
+    while (t < 256 && (int64_t)t * W < K) t *= 2;
+    return t;
 }
 
 struct GradLayout {
@@ -283,7 +361,9 @@ GradLayout grad_layout(int64_t N, int64_t K, int64_t V) {
     o = up(o + (size_t)(V + 1) * 4);
     b.ldpart = (K + 7) / 8 * 8;
     b.part = o;
-    o = up(o + (size_t)((N + RUN_BLOCK - 1) / RUN_BLOCK) * 2 * b.ldpart * 4);
+    // for either type's blocks
+    const int64_t places = std::min(run_places(N, K, row_threads(K, 4), 4), run_places(N, K, row_threads(K, 8), 8));
+    o = up(o + (size_t)((N + places - 1) / places) * 2 * b.ldpart * 4);
     b.total = o;
     return b;
 }
@@ -299,19 +379,23 @@ hipError_t launch_backward(const int64_t* tokens, const E* dX, int64_t lddx, E* 
     float* part = (float*)(ws + b.part);
     // 256 workgroups of equal ranges, or more of SORT_BINS entries
     const int64_t bins = (V + 255) / 256 < SORT_BINS ? (V + 255) / 256 : SORT_BINS;
+    int bits = 0;
+    while (((int64_t)1 << bits) < bins) ++bits;
     hipLaunchKernelGGL(sort_tokens_kernel, dim3((unsigned)((V + bins - 1) / bins)), dim3(SORT_WAVES * 64), 0, stream,
-                       tokens, (int)N, (int)V, (int)bins, order, start);
+                       tokens, (int)N, (int)V, (int)bins, bits, order, start);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t runs = (N + RUN_BLOCK - 1) / RUN_BLOCK;
-    const int64_t zeros = accumulate ? 0 : (V + RUN_BLOCK - 1) / RUN_BLOCK;
-    const unsigned chunks = (unsigned)((K + 256 * W - 1) / (256 * W));
+    const int per_row = row_threads(K, W), groups = 256 / per_row, places = run_places(N, K, per_row, W);
+    const int64_t blocks = (N + places - 1) / places, runs = (blocks + groups - 1) / groups;
+    const int64_t zeros = accumulate ? 0 : (V + RUN_MOST - 1) / RUN_MOST;
+    const unsigned chunks = (unsigned)((K + per_row * W - 1) / (per_row * W));
     hipLaunchKernelGGL(reduce_runs_kernel<E>, dim3((unsigned)(runs + zeros), chunks), dim3(256), 0, stream, tokens, dX,
-                       lddx, dE, ldde, K, (int)V, scale, accumulate ? 1 : 0, order, start, part, b.ldpart, (int)runs);
+                       lddx, dE, ldde, K, (int)V, scale, accumulate ? 1 : 0, order, start, part, b.ldpart, (int)runs,
+                       places, per_row);
     e = hipGetLastError();
-    if (e != hipSuccess || runs < 2) return e;
-    hipLaunchKernelGGL(join_runs_kernel<E>, dim3((unsigned)(runs - 1), chunks), dim3(256), 0, stream, tokens, dE, ldde,
-                       K, (int)V, scale, accumulate ? 1 : 0, order, start, part, b.ldpart);
+    if (e != hipSuccess || blocks < 2) return e;
+    hipLaunchKernelGGL(join_runs_kernel<E>, dim3((unsigned)(blocks - 1), chunks), dim3(JOIN_THREADS), 0, stream, tokens,
+                       dE, ldde, K, (int)V, scale, accumulate ? 1 : 0, order, start, part, b.ldpart, places, per_row);
     return hipGetLastError();
 }
 

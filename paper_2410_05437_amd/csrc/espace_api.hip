@@ -768,17 +768,20 @@ GemmArgs f32_args(const void* A, int64_t lda, const void* B, int64_t ldb, void* 
 
 }  // namespace
 
-// The cheapest of 256 x 256 and 256 x 192 tiles, priced as in plan_tiled_one, and the
-// small tiles, with up to `ranges` depth ranges.  tile -1: small tiles (config).
-struct F32Plan { int tile = -1, config = 0, ranges = 1; };
-
-static F32Plan f32_plan(int R, int Cc, int D, int64_t lda, int64_t ldb, int ranges) {
+F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges) {
     const int64_t lim = (int64_t)1 << 31;
     const int cus = device_cus();
     const double byte_cost = 315.0 / (2.0 * 64 * cus);
     F32Plan p;
+    if (use_gemv((int)R, (int)Cc, (int)D)) {
+        p.kind = F32Plan::GEMV;
+        return p;
+    }
     double best = 1e300;
-    if (espace::mid_supported(lda, ldb)) best = espace::mid_plan(R, Cc, D, cus, ranges, &p.config, &p.ranges);
+    if (espace::mid_supported(lda, ldb)) {
+        p.kind = F32Plan::MID;
+        best = espace::mid_plan((int)R, (int)Cc, (int)D, cus, ranges, &p.tile, &p.ranges);
+    }
     if (R * lda >= lim || Cc * ldb >= lim) return p;
     const int ktiles = ceil_div(D, 64);
     for (const int bn : {256, 192})
@@ -788,15 +791,11 @@ static F32Plan f32_plan(int R, int Cc, int D, int64_t lda, int64_t ldb, int rang
             if (s > 1) c += 97e3 + 1.37 * s * (double)R * Cc * 4.0 * byte_cost;
             if (4.75 + kUnitUs * c >= best) continue;
             best = 4.75 + kUnitUs * c;
+            p.kind = F32Plan::TILED;
             p.tile = bn == 256 ? espace::TILE_256x256 : espace::TILE_256x192;
             p.ranges = s;
         }
     return p;
-}
-
-int f32_tile(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb) {
-    if (use_gemv((int)R, (int)Cc, (int)D)) return -1;
-    return f32_plan((int)R, (int)Cc, (int)D, lda, ldb, 1).tile;
 }
 
 espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
@@ -806,30 +805,34 @@ espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb,
     if (!made) made = &one;
     *made = 1;
     if (dt == ESPACE_F32) {
-        e = espace::launch_gemm_tn_f32((const float*)A, lda, (const float*)B, ldb, C, ldc, (int)R, (int)Cc, (int)D,
-                                       device_cus(), stream);
+        e = espace::launch_gemm_tn_f32_ranges((const float*)A, lda, (const float*)B, ldb, C, ldc, (int)R, (int)Cc,
+                                              (int)D, device_cus(), ranges, made, stream);
     } else {
         GemmArgs g = f32_args(A, lda, B, ldb, C, ldc, R, Cc, D);
-        if (use_gemv((int)R, (int)Cc, (int)D)) {
-            e = espace::launch_gemv_tn_bf16(g, stream);
-        } else {
-            const F32Plan p = f32_plan((int)R, (int)Cc, (int)D, lda, ldb, ranges);
-            g.splits = p.ranges;
-            if (p.tile >= 0) {
-                g.tile = p.tile;
-                e = espace::launch_gemm_tn_bf16_v3_ranges(g, false, made, stream);
-            } else if (espace::mid_supported(lda, ldb)) {
-                g.tile = p.config;
-                *made = p.ranges;
-                e = espace::launch_mid_tn_bf16(g, stream);
-            } else {
+        const F32Plan p = f32_plan(R, Cc, D, lda, ldb, ranges);
+        g.tile = p.tile;
+        g.splits = *made = p.ranges;
+        switch (p.kind) {
+            case F32Plan::GEMV: e = espace::launch_gemv_tn_bf16(g, stream); break;
+            case F32Plan::MID: e = espace::launch_mid_tn_bf16(g, stream); break;
+            case F32Plan::TILED: e = espace::launch_gemm_tn_bf16_v3_ranges(g, false, made, stream); break;
+            default:
                 // matrices of 2^31 elements or more: the kernel with 64-bit offsets
                 g.tile = espace::TILE_128x128;
-                g.splits = 1;
                 e = espace::launch_gemm_tn_bf16(g, stream);
-            }
         }
     }
+    if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
+    return ESPACE_OK;
+}
+
+espace_status run_tn_scaled_mid(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
+                                int64_t R, int64_t Cc, int64_t D, int config, const float* scale, hipStream_t stream) {
+    GemmArgs g = f32_args(A, lda, B, ldb, C, ldc, R, Cc, D);
+    g.c_f32 = 0;
+    g.tile = config;
+    g.scale = scale;
+    const hipError_t e = espace::launch_mid_tn_bf16(g, stream);
     if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
     return ESPACE_OK;
 }

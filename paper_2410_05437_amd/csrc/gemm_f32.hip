@@ -64,7 +64,14 @@ constexpr int TK = 32;                            // depth step: 128-byte rows
 template <int BM, int BN>
 __global__ __launch_bounds__(256, 2)
 void gemm_tn_f32_mfma_kernel(const float* __restrict__ A, int64_t lda, const float* __restrict__ B, int64_t ldb,
-                             float* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c) {
+                             float* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c, int per_range,
+                             int64_t stride) {
+    // depth range blockIdx.y: per_range elements, a multiple of TK; its sums `stride` on
+    const int first = blockIdx.y * per_range;
+    A += first;
+    B += first;
+    C += blockIdx.y * stride;
+    D = min(D - first, per_range);
     constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
     constexpr int STAGE = (BM + BN) * TK * 4;
     constexpr int LPW = (BM + BN) / 8 / 4;        // 1 KB loads (8 rows) per wave and stage
@@ -247,7 +254,7 @@ hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64
     const int few = R < Cc ? R : Cc;
     auto tiled = [&](auto kernel, int t) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)tiles(t)), dim3(256), 0, stream, A, lda, B, ldb, C, ldc, R, Cc, D,
-                           (Cc + t - 1) / t);
+                           (Cc + t - 1) / t, D, (int64_t)0);
         return hipGetLastError();
     };
     // one launch unless its 512-thread workgroups were 2^32 threads, a launch's limit
@@ -289,6 +296,44 @@ hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64
     if (fits && tiles(64) >= cus / 2) return tiled(gemm_tn_f32_mfma_kernel<64, 64>, 64);
     if (tiles(32) >= 5 * (int64_t)cus / 8) return split(gemm_tn_f32_split_kernel<32, 8, 4>, 32);
     return split(gemm_tn_f32_split_kernel<16, 8, 4>, 16);
+}
+
+// Tiles of 128 or 64 and depth ranges by their estimated time: the matrix cores' 133
+// TFLOP/s on the tiles of the fullest CU, a launch and its ramp 8 us, and the sums
+// written and read again.  us with one range by the rules above -> with the cheapest:
+// 601 x 1000 x 5003 90 -> 61, 5003 x 1000 x 601 87 -> 70, 275 x 256 x 15712 112 -> 42.
+hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B, int64_t ldb, float* C, int64_t ldc,
+                                     int R, int Cc, int D, int cus, int ranges, int* made, hipStream_t stream) {
+    *made = 1;
+    const bool fits = (lda > ldb ? lda : ldb) * 128 * 4 < ((int64_t)1 << 32);
+    if (!fits || (R < Cc ? R : Cc) <= 32)
+        return launch_gemm_tn_f32(A, lda, B, ldb, C, ldc, R, Cc, D, cus, stream);
+    double best = 1e300;
+    int tile = 64;
+    for (const int t : {64, 128}) {
+        const int64_t tiles = (int64_t)((R + t - 1) / t) * ((Cc + t - 1) / t);
+        for (int s = 1; s <= ranges && (s == 1 || D / s >= 128); ++s) {
+            const int64_t rounds = (tiles * s + cus - 1) / cus;
+            const double us = rounds * (2.0 * t * t * D / s) / (133e6 / 256) + 8.0 +
+                              (s > 1 ? 2.0 * s * R * (double)Cc * 4 / 4e6 : 0.0);
+            if (us < best) {
+                best = us;
+                tile = t;
+                *made = s;
+            }
+        }
+    }
+    const int per = ((D + *made - 1) / *made + TK - 1) / TK * TK;
+    *made = (D + per - 1) / per;
+    const int64_t tr = (R + tile - 1) / tile, tc = (Cc + tile - 1) / tile;
+    const dim3 grid((unsigned)(tr * tc), (unsigned)*made);
+    if (tile == 128)
+        hipLaunchKernelGGL((gemm_tn_f32_mfma_kernel<128, 128>), grid, dim3(256), 0, stream, A, lda, B, ldb, C, ldc, R, Cc,
+                           D, (int)tc, per, (int64_t)R * ldc);
+    else
+        hipLaunchKernelGGL((gemm_tn_f32_mfma_kernel<64, 64>), grid, dim3(256), 0, stream, A, lda, B, ldb, C, ldc, R, Cc,
+                           D, (int)tc, per, (int64_t)R * ldc);
+    return hipGetLastError();
 }
 
 }  // namespace espace

@@ -50,6 +50,7 @@ struct GemmArgs {
     // one whole cache line.  ld (elements per row pair) is a multiple of 64.
     int a_pairs = 0;    // A is in the row-pair layout (lda its pair pitch)
     int c_pairs = 0;    // write C (bf16) in the row-pair layout (ldc its pair pitch)
+    const float* scale = nullptr;   // small tiles in one range: C = scale[0] * sums, rounded
 };
 
 // Whether all XCDs walk the depth of a tiled product in one order (DepthOrder of
@@ -163,6 +164,10 @@ hipError_t launch_splitk_reduce(const float* P, int S, int64_t split_stride, int
                                 hipStream_t stream);
 hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64_t ldb,
                               float* C, int64_t ldc, int R, int Cc, int D, int cus, hipStream_t stream);
+// The same in up to `ranges` depth ranges, *made of them, R * ldc apart in C; not
+// combined.
+hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B, int64_t ldb, float* C, int64_t ldc,
+                                     int R, int Cc, int D, int cus, int ranges, int* made, hipStream_t stream);
 
 // fp32 sums of the depth ranges of a 256 x 256 or 256 x 192 tiled product
 // (g.splits ranges requested; *ranges receives the number of non-empty ones),

@@ -163,16 +163,23 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict_
 
 // ---- forward -------------------------------------------------------------------
 
+// four logits, from the first slab's address
+__device__ __forceinline__ f32x4_t logits4(const float* p, const Logits& S) {
+    f32x4_t x = *reinterpret_cast<const f32x4_t*>(p);
+    for (int s = 1; s < S.slabs; ++s) x += *reinterpret_cast<const f32x4_t*>(p + s * S.stride);
+    return x;
+}
+
 // STAT_COLS columns of one token: 256 threads of 4 x 4 columns each, kept in
 // registers between the maximum and the sum.
-__global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S, int64_t lds, int c0, int cols,
+__global__ __launch_bounds__(256) void stats_kernel(Logits S, int c0, int cols,
                                                     float inv_t, LossTargets t, float2* __restrict__ part, int N,
                                                     int part0, int n0, float* __restrict__ picked, int64_t ldpk) {
     __shared__ float red[8];
     const int n = n0 + blockIdx.y;
     const int b0 = blockIdx.x * STAT_COLS;
     const int left = cols - b0 < STAT_COLS ? cols - b0 : STAT_COLS;
-    const float* row = S + (int64_t)n * lds + b0;
+    const float* row = S.S + (int64_t)n * S.lds + b0;
     float v[4][4];
     float m = -INFINITY;
 #pragma unroll
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S,
         const int c = i * 1024 + threadIdx.x * 4;
         // rows are padded to a multiple of 8 columns
         f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-        if (c < left) x = *reinterpret_cast<const f32x4_t*>(row + c);
+        if (c < left) x = logits4(row + c, S);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             v[i][e] = c + e < left ? x[e] * inv_t : -INFINITY;
@@ -208,7 +215,11 @@ __global__ __launch_bounds__(256) void stats_kernel(const float* __restrict__ S,
     }
     for (int j = threadIdx.x; j < t.T; j += 256) {
         const int64_t c = (t.labels ? t.labels[n] : (int64_t)t.col[(int64_t)n * t.T + j]) - c0 - b0;
-        if (c >= 0 && c < left) picked[(int64_t)n * ldpk + j] = row[c] * inv_t;
+        if (c >= 0 && c < left) {
+            float x = row[c];
+            for (int s = 1; s < S.slabs; ++s) x += row[c + s * S.stride];
+            picked[(int64_t)n * ldpk + j] = x * inv_t;
+        }
     }
 }
 
@@ -306,7 +317,7 @@ __device__ __forceinline__ float zero_of(float) { return 0.f; }
 
 // 64 x 64 of G, its transpose through LDS.  Term 1 is what term 0's rounding left.
 template <typename E>
-__global__ __launch_bounds__(256) void grad_kernel(const float* __restrict__ S, int64_t lds, int N, int c0, int cols,
+__global__ __launch_bounds__(256) void grad_kernel(Logits S, int N, int c0, int cols,
                                                    float inv_t, const float* __restrict__ lse,
                                                    const float* __restrict__ r, const int64_t* __restrict__ labels,
                                                    GradOut out) {
@@ -321,7 +332,7 @@ __global__ __launch_bounds__(256) void grad_kernel(const float* __restrict__ S, 
         for (int e = 0; e < 4; ++e) g[i][e] = 0.f;
         if (n >= N || c >= cols) continue;
         const float rn = r[n];
-        const f32x4_t s = *reinterpret_cast<const f32x4_t*>(S + (int64_t)n * lds + c);
+        const f32x4_t s = logits4(S.S + (int64_t)n * S.lds + c, S);
         const float ls = lse[n];
         const int64_t at = labels ? labels[n] - c0 - c : -1;
 #pragma unroll
@@ -483,14 +494,14 @@ hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits
     return hipGetLastError();
 }
 
-hipError_t launch_loss_stats(const float* S, int64_t lds, int N, int c0, int cols, float inv_t,
+hipError_t launch_loss_stats(const Logits& S, int N, int c0, int cols, float inv_t,
                              const LossTargets& t, float2* part, int part0, float* picked, int64_t ldpk,
                              hipStream_t stream) {
     // a launch has at most 65535 workgroups in y
     const int chunks = (cols + STAT_COLS - 1) / STAT_COLS;
     for (int n0 = 0; n0 < N; n0 += 65535) {
         const int rows = N - n0 < 65535 ? N - n0 : 65535;
-        hipLaunchKernelGGL(stats_kernel, dim3(chunks, rows), dim3(256), 0, stream, S, lds, c0, cols, inv_t, t, part, N,
+        hipLaunchKernelGGL(stats_kernel, dim3(chunks, rows), dim3(256), 0, stream, S, c0, cols, inv_t, t, part, N,
                            part0, n0, picked, ldpk);
     }
     return hipGetLastError();
@@ -512,13 +523,13 @@ hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const flo
 // N < 2^22 tokens: at most 65536 workgroups of 64 rows in y
 static_assert((1 << 22) / 64 <= 65536, "launch limit");
 
-hipError_t launch_loss_grad(const float* S, int64_t lds, int N, int c0, int cols, float inv_t, const float* lse,
+hipError_t launch_loss_grad(const Logits& S, int N, int c0, int cols, float inv_t, const float* lse,
                             const float* r, const int64_t* labels, const GradOut& out, hipStream_t stream) {
     const dim3 grid((cols + 63) / 64, (N + 63) / 64), block(256);
     if (out.f32)
-        hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S, lds, N, c0, cols, inv_t, lse, r, labels, out);
+        hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S, N, c0, cols, inv_t, lse, r, labels, out);
     else
-        hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S, lds, N, c0, cols, inv_t, lse, r, labels,
+        hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S, N, c0, cols, inv_t, lse, r, labels,
                            out);
     return hipGetLastError();
 }

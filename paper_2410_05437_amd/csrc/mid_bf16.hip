@@ -106,7 +106,8 @@ template <int BM, int BN, int W, int ST, int SEG>
 __global__ __launch_bounds__(W * 64, W / 4)
 void mid_tn_bf16_kernel(const uint16_t* __restrict__ A, int64_t lda, const uint16_t* __restrict__ B, int64_t ldb,
                         uint16_t* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c, int c_pairs,
-                        float* __restrict__ part, int64_t ldp, int64_t split_stride, int sps, int upper) {
+                        float* __restrict__ part, int64_t ldp, int64_t split_stride, int sps, int upper,
+                        const float* __restrict__ scale) {
     using T = MidCfg<BM, BN, W, ST, SEG>;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[T::SMEM];
     int tile_r, tile_c;
@@ -251,6 +252,7 @@ void mid_tn_bf16_kernel(const uint16_t* __restrict__ A, int64_t lda, const uint1
             *reinterpret_cast<f32x4_t*>(part + blockIdx.y * split_stride + (int64_t)r * ldp + c) = v;
             continue;
         }
+        if (scale) v *= scale[0];
         // c is a multiple of 4: the run stays inside one 32-column block of
         // the row-pair layout
         uint16_t* p = C + (c_pairs ? pair_offset(r, c, ldc) : (int64_t)r * ldc + c);
@@ -273,7 +275,7 @@ hipError_t launch_cfg_mid(const GemmArgs& g, bool upper, hipStream_t stream) {
     hipLaunchKernelGGL((mid_tn_bf16_kernel<BM, BN, W, ST, SEG>), dim3(tr * tc, S), dim3(W * 64), 0, stream, g.A,
                        g.lda, g.B, g.ldb, (uint16_t*)g.C, g.ldc, g.R, g.Cc, g.D, tc, g.c_pairs,
                        S > 1 || upper || g.c_f32 ? g.partial : nullptr, ldp, stride, (steps + S - 1) / S,
-                       upper ? 1 : 0);
+                       upper ? 1 : 0, g.scale);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || S == 1 || upper || g.c_f32) return e;
     return launch_splitk_reduce(g.partial, S, stride, ldp, g.C, g.ldc, g.R, g.Cc, g.c_pairs ? 2 : 1, stream);
@@ -340,7 +342,7 @@ static hipError_t launch_config(const GemmArgs& g, bool upper, hipStream_t strea
 }
 
 hipError_t launch_mid_tn_bf16(const GemmArgs& g, hipStream_t stream) {
-    if (!mid_supported(g.lda, g.ldb) || g.a_pairs) return hipErrorInvalidValue;
+    if (!mid_supported(g.lda, g.ldb) || g.a_pairs || (g.scale && (g.splits > 1 || g.c_f32))) return hipErrorInvalidValue;
     if (g.c_f32 && (g.C != g.partial || g.ldc != splitk_ld(g.Cc))) return hipErrorInvalidValue;
     return launch_config(g, false, stream);
 }

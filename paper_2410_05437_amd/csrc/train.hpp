@@ -43,10 +43,17 @@ struct TeacherOut {
 hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits, int64_t ldl, int N, int T, int V,
                           float inv_t, const TeacherOut& out, hipStream_t stream);
 
-// Columns [c0, c0 + cols) of the logits, S [N][lds] float32: the largest s / t and Σ
+// Logits as float32 sums: `slabs` of them, `stride` apart, to be added in order.
+struct Logits {
+    const float* S = nullptr;
+    int64_t lds = 0;
+    int slabs = 1;
+    int64_t stride = 0;
+};
+// Columns [c0, c0 + cols) of the logits of N tokens: the largest s / t and Σ
 // exp(s / t - it) of every STAT_COLS of them at part[k][n] (k from part0 on), and s / t
 // of the targets among them at picked[n][j].
-hipError_t launch_loss_stats(const float* S, int64_t lds, int N, int c0, int cols, float inv_t,
+hipError_t launch_loss_stats(const Logits& S, int N, int c0, int cols, float inv_t,
                              const LossTargets& t, float2* part, int part0, float* picked, int64_t ldpk,
                              hipStream_t stream);
 // loss and lse from the nparts parts of each token; picked of empty places.
@@ -69,9 +76,9 @@ struct GradOut {
     int terms = 1;
     bool f32 = false;
 };
-// G of columns [c0, c0 + cols) from S; labels may be NULL (their entries are
+// G of columns [c0, c0 + cols) from their logits; labels may be NULL (their entries are
 // launch_loss_fix's).
-hipError_t launch_loss_grad(const float* S, int64_t lds, int N, int c0, int cols, float inv_t, const float* lse,
+hipError_t launch_loss_grad(const Logits& S, int N, int c0, int cols, float inv_t, const float* lse,
                             const float* r, const int64_t* labels, const GradOut& out, hipStream_t stream);
 // The teacher's entries among these columns, from their logits `picked`.
 hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ldpk, const float* lse, const float* r,

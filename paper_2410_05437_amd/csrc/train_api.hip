@@ -16,7 +16,7 @@ namespace {
 
 using espace::LossTargets;
 
-constexpr int64_t kMaxTokens = (int64_t)1 << 21;
+constexpr int64_t kMaxTokens = (int64_t)1 << 21, kMaxWidth = (int64_t)1 << 21;
 
 int64_t ld8(int64_t c) { return (c + 7) / 8 * 8; }
 
@@ -45,9 +45,26 @@ constexpr int64_t kNarrow = 256;
 // 2.4e-3 off, 1.7e-3 with two, the rounding of the results), and the products of so few
 // are bound by reading W.
 constexpr int64_t kTwoTerms = 128;
-// Depth ranges of dX's product, left to the pass that rounds it, and the floats of
-// their sums.
+// Depth ranges of the logits' and dX's products whose sums the next pass adds, and the
+// floats of them.
 constexpr int64_t kRanges = 16, kRangeFloats = (int64_t)1 << 24;
+
+int most_ranges(int64_t R, int64_t ld) { return (int)std::max<int64_t>(1, std::min(kRanges, kRangeFloats / (R * ld))); }
+
+// How a gradient's product ends: from the tiles' epilogue (its `tile`), from the small
+// tiles' (their configuration), or as float32 sums that a pass of their own rounds.
+struct End {
+    enum { SUMS, EPILOGUE, SMALL } how = SUMS;
+    int tile = -1;
+};
+End end_of(const F32Plan& p) {
+    End e;
+    if (p.ranges == 1 && (p.kind == F32Plan::TILED || p.kind == F32Plan::MID)) {
+        e.how = p.kind == F32Plan::TILED ? End::EPILOGUE : End::SMALL;
+        e.tile = p.tile;
+    }
+    return e;
+}
 
 struct Layout {
     size_t S, part, picked, col, p, logp, sorted, place, first;    // forward (S, col, p: both)
@@ -56,8 +73,8 @@ struct Layout {
     int slab;                    // columns of their slabs
     int64_t P;                   // columns of a piece
     int terms;
-    int tile_x, tile_w;          // >= 0: dX, dW from the gradients' epilogue
-    int ranges;                  // of dX's product otherwise
+    End x, w;                    // of dX's and dW's products
+    int ranges_s, ranges_x;      // of the logits' (tile < 0) and dX's (sums) products, at most
     int64_t ldn, ldp, ldk, ldfirst;
 };
 
@@ -73,10 +90,18 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     };
     b.terms = bf16 && N <= kTwoTerms ? 2 : 1;
     b.P = backward ? piece_cols(N, V, kGrads) : V;
-    b.tile = bf16 && b.terms == 1 ? f32_tile(N, b.P, K, ld8(K), ld8(K)) : -1;
-    if (b.tile < 0) b.P = piece_cols(N, V, kLogits);
+    b.tile = -1;
+    if (bf16 && b.terms == 1) {
+        const F32Plan p = f32_plan(N, b.P, K, ld8(K), ld8(K), 1);
+        if (p.kind == F32Plan::TILED) b.tile = p.tile;
+    }
+    b.ranges_s = 1;
+    if (b.tile < 0) {
+        b.P = piece_cols(N, V, kLogits);
+        b.ranges_s = most_ranges(N, espace::splitk_ld((int)b.P));
+    }
     b.slab = espace::loss_slab(b.tile);
-    b.S = take((size_t)N * espace::splitk_ld((int)(b.tile < 0 ? b.P : std::min(V, kNarrow))) * 4);
+    b.S = take((size_t)N * espace::splitk_ld((int)(b.tile < 0 ? b.P : std::min(V, kNarrow))) * 4 * b.ranges_s);
     if (T > 0) {
         b.col = take((size_t)N * T * 4);
         b.p = take((size_t)N * T * 4);
@@ -110,29 +135,30 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     b.G = take((size_t)N * b.terms * b.ldp * es);
     b.GT = take((size_t)b.P * b.ldn * b.terms * es);
     b.WT = take((size_t)K * b.ldp * es);
-    b.tile_x = b.tile_w = -1;
-    if (b.tile >= 0) {
-        // each gradient's sums from its own epilogue, dX's unless its tiles leave most
-        // CUs without one and ranges of the depth can be summed later
-        b.tile_x = f32_tile(N, K, b.P, b.ldp, b.ldp);
-        b.tile_w = f32_tile(b.P, K, N, b.ldn, b.ldn);
-        const int64_t tiles = (N + 255) / 256 * ((K + 255) / 256);
-        if (pieces <= 4 && 2 * tiles < device_cus()) b.tile_x = -1;
+    const int64_t rows = N * b.terms;
+    b.ranges_x = pieces <= 4 ? most_ranges(rows, b.ldk) : 1;
+    if (bf16) {
+        b.w = end_of(f32_plan(b.P, K, b.ldn * b.terms, b.ldn * b.terms, b.ldn * b.terms, 1));
+        if (b.terms == 1) b.x = end_of(f32_plan(N, K, b.P, b.ldp, b.ldp, b.ranges_x));
+        // the small tiles do not add to what is there
+        if (b.x.how == End::SMALL && pieces > 1) b.x = End{};
     }
-    // without the epilogue: the ranges of up to 4 pieces, or two float32 sums
-    b.ranges = (int)std::max<int64_t>(1, std::min(kRanges, kRangeFloats / (N * b.terms * b.ldk)));
-    const int64_t sums = b.tile_x >= 0 ? (pieces > 1 ? 1 : 0) : (pieces <= 4 && bf16 ? b.ranges * pieces : std::min<int64_t>(pieces, 2));
-    // (a call whose leading dimensions take it to narrow pieces has two)
-    b.acc = take((size_t)N * b.terms * b.ldk * 4 * std::max<int64_t>(sums, b.tile >= 0 ? 2 : 1));
-    b.out = take((size_t)(b.tile_w >= 0 ? std::min(V, kNarrow) : b.P) * b.ldk * 4);
+    // sums of dX: of more than one piece to be added to, or ranges, or two pieces'; a
+    // call whose leading dimensions take it to narrow pieces has two
+    int64_t sums = std::min<int64_t>(pieces, 2);
+    if (b.x.how != End::SUMS) sums = pieces > 1 ? 1 : 0;
+    else if (pieces <= 4) sums = b.ranges_x * pieces;
+    if (b.tile >= 0) sums = std::max<int64_t>(sums, 2);
+    b.acc = take((size_t)rows * b.ldk * 4 * sums);
+    b.out = take((size_t)(b.w.how != End::SUMS ? std::min(V, kNarrow) : b.P) * b.ldk * 4);
     b.total = o;
     return b;
 }
 
 espace_status check_sizes(int64_t N, int64_t K, int64_t V) {
     if (N < 0 || N >= kMaxTokens) return fail(ESPACE_ERR_SHAPE, "need 0 <= N < 2^21 tokens (N=%lld)", (long long)N);
-    if (K < 1 || K > kMaxDim || V < 1 || V > kMaxDim)
-        return fail(ESPACE_ERR_SHAPE, "need 1 <= K, V <= 2^30 (K=%lld, V=%lld)", (long long)K, (long long)V);
+    if (K < 1 || K > kMaxWidth || V < 1 || V > kMaxDim)
+        return fail(ESPACE_ERR_SHAPE, "need 1 <= K <= 2^21 and 1 <= V <= 2^30 (K=%lld, V=%lld)", (long long)K, (long long)V);
     return ESPACE_OK;
 }
 
@@ -193,18 +219,22 @@ const int64_t kLim = (int64_t)1 << 31;
 
 // columns [c0, c0 + cols) of the logits, float32
 espace_status logits_piece(const void* X, int64_t ldx, const void* W, int64_t ldw, float* S, int64_t N, int64_t K,
-                           int64_t c0, int64_t cols, espace_dtype dt, hipStream_t stream) {
-    return run_tn_f32(X, ldx, (const char*)W + (size_t)c0 * ldw * elem_size(dt), ldw, S,
-                      espace::splitk_ld((int)cols), N, cols, K, dt, stream);
+                           int64_t c0, int64_t cols, espace_dtype dt, int ranges, espace::Logits* out,
+                           hipStream_t stream) {
+    out->S = S;
+    out->lds = espace::splitk_ld((int)cols);
+    out->stride = N * out->lds;
+    return run_tn_f32(X, ldx, (const char*)W + (size_t)c0 * ldw * elem_size(dt), ldw, S, out->lds, N, cols, K, dt,
+                      stream, ranges, &out->slabs);
 }
 
 void log_plan(const Layout& b, bool backward, bool fused, int64_t N, int64_t K, int64_t V, int64_t T, int64_t P) {
     if (!plan_log()) return;
     std::fprintf(stderr,
                  "espace loss plan N=%lld K=%lld V=%lld T=%lld: backward=%d fused=%d tile=%d columns=%lld terms=%d "
-                 "tile_x=%d tile_w=%d ranges=%d\n",
+                 "x=%d w=%d ranges_s=%d ranges_x=%d\n",
                  (long long)N, (long long)K, (long long)V, (long long)T, backward, fused, b.tile, (long long)P, b.terms,
-                 b.tile_x, b.tile_w, b.ranges);
+                 (int)b.x.how, (int)b.w.how, b.ranges_s, b.ranges_x);
 }
 
 espace_status loss_forward(const void* X, int64_t ldx, const void* W, int64_t ldw, LossTargets t, float* loss,
@@ -244,10 +274,10 @@ espace_status loss_forward(const void* X, int64_t ldx, const void* W, int64_t ld
         const int64_t P = b.tile >= 0 ? std::min(V, kNarrow) : b.P;
         for (int64_t c0 = 0; c0 < V; c0 += P) {
             const int64_t cols = std::min(P, V - c0);
-            ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, stream));
-            ESPACE_LAUNCH("loss statistics",
-                          espace::launch_loss_stats(S, espace::splitk_ld((int)cols), (int)N, (int)c0, (int)cols, inv_t,
-                                                    t, part, parts, picked, ldpk, stream));
+            espace::Logits s;
+            ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, b.ranges_s, &s, stream));
+            ESPACE_LAUNCH("loss statistics", espace::launch_loss_stats(s, (int)N, (int)c0, (int)cols, inv_t, t, part,
+                                                                       parts, picked, ldpk, stream));
             parts += (int)((cols + espace::STAT_COLS - 1) / espace::STAT_COLS);
         }
     }
@@ -270,12 +300,13 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     void *XT = ws + b.XT, *G = ws + b.G, *GT = ws + b.GT, *WT = ws + b.WT;
     const float inv_t = 1.f / temperature;
     const bool fused = b.tile >= 0 && N * ldx < kLim && b.P * ldw < kLim;
-    const int tile_x = fused ? b.tile_x : -1, tile_w = fused ? b.tile_w : -1;
-    const int64_t P = b.tile >= 0 && !fused ? std::min(V, kNarrow) : b.P;
+    // leading dimensions past the epilogues' offsets: narrow pieces and float32 sums
+    const bool narrow = b.tile >= 0 && !fused;
+    const int64_t P = narrow ? std::min(V, kNarrow) : b.P;
     const int64_t pieces = (V + P - 1) / P;
+    const End ex = narrow ? End{} : b.x, ew = narrow ? End{} : b.w;
     const int64_t rows = N * b.terms, slab = rows * b.ldk;      // of dX's sums
-    const bool many = tile_x < 0 && pieces <= 4 && !f32 && !(b.tile >= 0 && !fused);
-    const int ranges = many ? b.ranges : 1;
+    const bool many = pieces <= 4 && !narrow;                   // their ranges stay apart
     const int64_t ldgt = b.ldn * b.terms;
     int sums = 0;                                               // slabs in acc
     log_plan(b, true, fused, N, K, V, t.labels ? 0 : t.T, P);
@@ -305,10 +336,10 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             e.r = r;
             ESPACE_TRY(run_tn_loss(X, ldx, Wp, ldw, G, b.ldp, N, cols, K, b.tile, espace::LOSS_GRAD, e, stream));
         } else {
-            ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, stream));
-            ESPACE_LAUNCH("logits' gradient",
-                          espace::launch_loss_grad(S, espace::splitk_ld((int)cols), (int)N, (int)c0, (int)cols, inv_t,
-                                                   lse, r, t.labels, go, stream));
+            espace::Logits s;
+            ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, b.ranges_s, &s, stream));
+            ESPACE_LAUNCH("logits' gradient", espace::launch_loss_grad(s, (int)N, (int)c0, (int)cols, inv_t, lse, r,
+                                                                       t.labels, go, stream));
         }
         if (!t.labels)
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
@@ -317,38 +348,43 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             ESPACE_LAUNCH("transpose", espace::launch_transpose(G, b.ldp, (int)N, (int)cols, GT, b.ldn, f32, stream));
         if (dX) {
             ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, b.ldp, f32, stream));
-            if (tile_x >= 0) {
+            if (ex.how == End::EPILOGUE) {
                 espace::LossEpi e;
                 e.acc = acc;
                 e.ldacc = b.ldk;
                 e.scale = scale;
                 e.add = c0 > 0;
                 e.last = last;
-                ESPACE_TRY(run_tn_loss(G, b.ldp, WT, b.ldp, dX, lddx, N, K, cols, tile_x, espace::LOSS_GRAD_OUT, e,
+                ESPACE_TRY(run_tn_loss(G, b.ldp, WT, b.ldp, dX, lddx, N, K, cols, ex.tile, espace::LOSS_GRAD_OUT, e,
                                        stream));
+            } else if (ex.how == End::SMALL) {
+                ESPACE_TRY(run_tn_scaled_mid(G, b.ldp, WT, b.ldp, dX, lddx, N, K, cols, ex.tile, scale, stream));
             } else {
                 int made = 1;
-                ESPACE_TRY(run_tn_f32(G, b.ldp, WT, b.ldp, acc + sums * slab, b.ldk, rows, K, cols, dt, stream, ranges,
-                                      &made));
+                ESPACE_TRY(run_tn_f32(G, b.ldp, WT, b.ldp, acc + sums * slab, b.ldk, rows, K, cols, dt, stream,
+                                      many ? b.ranges_x : 1, &made));
                 if (many || !sums) sums += made;
                 else ESPACE_LAUNCH("sum", espace::launch_add_f32(acc, acc + slab, slab, stream));
             }
         }
         if (dW) {
             void* o = (char*)dW + (size_t)c0 * lddw * es;
-            if (tile_w >= 0) {
+            const int64_t depth = b.terms > 1 ? b.ldn + N : N;
+            if (ew.how == End::EPILOGUE) {
                 espace::LossEpi e;
                 e.scale = scale;
                 e.last = 1;
-                ESPACE_TRY(run_tn_loss(GT, ldgt, XT, ldgt, o, lddw, cols, K, N, tile_w, espace::LOSS_GRAD_OUT, e,
+                ESPACE_TRY(run_tn_loss(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ew.tile, espace::LOSS_GRAD_OUT, e,
                                        stream));
+            } else if (ew.how == End::SMALL) {
+                ESPACE_TRY(run_tn_scaled_mid(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ew.tile, scale, stream));
             } else {
-                ESPACE_TRY(run_tn_f32(GT, ldgt, XT, ldgt, out, b.ldk, cols, K, b.terms > 1 ? b.ldn + N : N, dt, stream));
+                ESPACE_TRY(run_tn_f32(GT, ldgt, XT, ldgt, out, b.ldk, cols, K, depth, dt, stream));
                 ESPACE_LAUNCH("gradient", espace::launch_sum_out(out, b.ldk, 1, 0, scale, o, lddw, cols, K, f32, stream));
             }
         }
     }
-    if (dX && tile_x < 0)
+    if (dX && ex.how == End::SUMS)
         // a second term's rows are a slab of their own
         ESPACE_LAUNCH("gradient", espace::launch_sum_out(acc, b.ldk, sums * b.terms, N * b.ldk, scale, dX, lddx, N, K,
                                                          f32, stream));
@@ -464,7 +500,7 @@ extern "C" {
 size_t espace_linear_loss_workspace_bytes(int backward, int64_t N, int64_t K, int64_t V, int64_t T,
                                           espace_dtype dt) {
     if (dt != ESPACE_F32 && dt != ESPACE_BF16) return SIZE_MAX;
-    if (N < 0 || N >= kMaxTokens || K < 1 || K > kMaxDim || V < 1 || V > kMaxDim) return SIZE_MAX;
+    if (N < 0 || N >= kMaxTokens || K < 1 || K > kMaxWidth || V < 1 || V > kMaxDim) return SIZE_MAX;
     if (T < 0 || T > ESPACE_MAX_TEACHER_ENTRIES) return SIZE_MAX;
     return N ? loss_layout(backward != 0, N, K, V, T, dt).total : 0;
 }
@@ -539,7 +575,7 @@ espace_status espace_embedding(const int64_t* tokens, const void* E, int64_t lde
 }
 
 size_t espace_embedding_workspace_bytes(int64_t N, int64_t K, int64_t V) {
-    if (N < 0 || N >= kMaxTokens || K < 1 || K > kMaxDim || V < 1 || V > kMaxDim) return SIZE_MAX;
+    if (N < 0 || N >= kMaxTokens || K < 1 || K > kMaxWidth || V < 1 || V > kMaxDim) return SIZE_MAX;
     return N ? align_ws(espace::embedding_workspace_bytes(N, K, V)) : 0;
 }
 

@@ -64,6 +64,7 @@ def test_loss_refusals():
     for call in (_ce, _ceb, _kd, _kdb):
         assert call(X=NULL) == 1 and call(W=NULL) == 1 and call(lse=NULL) == 1
         assert call(N=-1) == 2 and call(N=1 << 21) == 2 and call(K=0) == 2 and call(V=0) == 2 and call(V=1 << 31) == 2
+        assert call(K=1 << 22, ldx=1 << 22, ldw=1 << 22) == 2
         assert call(ldx=56) == 2 and call(ldw=56) == 2 and call(ldx=68) == 3
         assert call(X=off(P(1), 8)) == 3 and call(lse=off(P(5), 2)) == 3
         assert call(dt=2) == 4
