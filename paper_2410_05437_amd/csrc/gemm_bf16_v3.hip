@@ -38,7 +38,15 @@ namespace {
 
 struct V3NoEpi {};
 
-__device__ __forceinline__ float v3_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+// f over the four lanes that share a row (16 apart); every one gets the result
+template <class F>
+__device__ __forceinline__ float v3_over_row(float x, F f) {
+    const unsigned u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned w = __float_as_uint(f(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 // The rows of a wave's 128 x BN/2 sub-tile are spread as elsewhere: block (i, j), row
 // 16 i + lane % 16, columns 16 j + 4 (lane / 16) + {0..3}.  row0, col0: the sub-tile's
@@ -77,31 +85,33 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
             if (r >= R) q1[i] = 0;
             col[i] = q0[i] < q1[i] ? epi.col[(int64_t)r * entries + q0[i]] : 0;
         }
+        const bool whole = col0 + BN / 2 <= Cc;   // of the vocabulary
+        const float k = epi.inv_t * 1.44269504088896340736f;
 #pragma unroll
         for (int i = 0; i < V3_NB; ++i) {
             const int r = row0 + 16 * i + lr;
-            float v[NBJ][4];
+            f32x4_t v[NBJ];
             float m = -INFINITY;
 #pragma unroll
             for (int j = 0; j < NBJ; ++j) {
-                const f32x4_t a = v3_acc_read(acc[i][j]);
+                v[j] = v3_acc_read(acc[i][j]);
+                if (!whole)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[j][e] = c0 + 16 * j + e < Cc ? a[e] * epi.inv_t : -INFINITY;
-                    m = fmaxf(m, v[j][e]);
-                }
+                    for (int e = 0; e < 4; ++e) v[j][e] = c0 + 16 * j + e < Cc ? v[j][e] : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, v[j][e]);
             }
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
+            m = v3_over_row(m, [](float a, float b) { return fmaxf(a, b); });
+            // all -infinity: the sum stays 0, and NaN (which a maximum passes over) NaN
             const float base = m == -INFINITY ? 0.f : m;
             float l = 0.f;
 #pragma unroll
             for (int j = 0; j < NBJ; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) l += v3_exp(v[j][e] - base);
-            l += __shfl_xor(l, 16);
-            l += __shfl_xor(l, 32);
-            if (lh == 0 && r < R) epi.part[(int64_t)slab * R + r] = make_float2(l == 0.f ? -INFINITY : base, l);
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f((v[j][e] - base) * k);
+            l = v3_over_row(l, [](float a, float b) { return a + b; });
+            if (lh == 0 && r < R)
+                epi.part[(int64_t)slab * R + r] = make_float2(l == 0.f ? -INFINITY : base * epi.inv_t, l);
             if (epi.labels) {
                 if (__any(lab[i] >= 0) && lab[i] >= 0 && r < R && ((lab[i] >> 2) & 3) == lh) {
                     float x = 0.f;
@@ -109,7 +119,7 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
                     for (int j = 0; j < NBJ; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x = lab[i] == 16 * j + 4 * lh + e ? v[j][e] : x;
-                    epi.picked[(int64_t)r * epi.ldpk] = x;
+                    epi.picked[(int64_t)r * epi.ldpk] = x * epi.inv_t;
                 }
             } else if (entries && __any(q0[i] < q1[i])) {
                 // the wave's own LDS, in the order of its instructions; 16-byte chunk c
@@ -118,15 +128,14 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int j = 0; j < NBJ; ++j)
-                    *reinterpret_cast<f32x4_t*>(spare + lr * 128 + ((4 * j + lh) ^ lr) * 4) =
-                        f32x4_t{v[j][0], v[j][1], v[j][2], v[j][3]};
+                    *reinterpret_cast<f32x4_t*>(spare + lr * 128 + ((4 * j + lh) ^ lr) * 4) = v[j];
                 __builtin_amdgcn_wave_barrier();
                 int q = q0[i], c = col[i];
                 while (__any(q < q1[i])) {
                     if (q < q1[i]) {
                         const int at = min(max(c - epi.col0 - col0, 0), BN / 2 - 1);
                         epi.picked[(int64_t)r * epi.ldpk + epi.place[(int64_t)r * entries + q]] =
-                            spare[lr * 128 + ((at >> 2) ^ lr) * 4 + (at & 3)];
+                            spare[lr * 128 + ((at >> 2) ^ lr) * 4 + (at & 3)] * epi.inv_t;
                     }
                     q += 4;
                     c = q < q1[i] ? epi.col[(int64_t)r * entries + q] : 0;
@@ -162,30 +171,74 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
                     lab[i] = c >= 0 && c < BN ? (int)c : -1;
                 }
             }
+            const bool whole = col0 + BN / 2 <= Cc;
+            const float k = epi.inv_t * 1.44269504088896340736f;
+            unsigned* turn = reinterpret_cast<unsigned*>(spare);
+            const unsigned pick = (lr & 1) ? 0x03020706u : 0x05040100u;
 #pragma unroll
-            for (int i = 0; i < V3_NB; ++i) {
-                const int r = row0 + 16 * i + lr;
-                auto value = [&](int j) -> f32x4_t {
-                    const f32x4_t a = v3_acc_read(acc[i][j]);
-                    f32x4_t g;
+            for (int h = 0; h < V3_NB / 2; ++h) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float x = v3_exp(a[e] * epi.inv_t - ls[i]);
-                        x = lab[i] == 16 * j + e ? x - 1.f : x;
+                for (int ii = 0; ii < 2; ++ii) {
+                    const int i = 2 * h + ii, r = row0 + 16 * i + lr;
+                    const float shift = ls[i] * 1.44269504088896340736f;
+                    const unsigned live = rn[i] == 0.f ? 0u : 0xffffffffu;
+                    const bool labelled = __any(lab[i] >= 0 && lab[i] < BN / 2);
+                    unsigned w[NBJ][2];
+#pragma unroll
+                    for (int j = 0; j < NBJ; ++j) {
+                        f32x4_t x = v3_acc_read(acc[i][j]);
+                        // the exponent's rounding, 2^-24 of |s| + |lse|, is far below bfloat16's
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], k, -shift));
+                        if (labelled)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[e] = lab[i] == 16 * j + e ? x[e] - 1.f : x[e];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] *= rn[i];
+                        if (!whole)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[e] = c0 + 16 * j + e < Cc ? x[e] : 0.f;
                         // a token without a target: 0 whatever its logits are
-                        x = rn[i] == 0.f ? 0.f : rn[i] * x;
-                        g[e] = c0 + 16 * j + e < Cc ? x : 0.f;
+                        w[j][0] = pack_bf16x2(x[0], x[1]) & live;
+                        w[j][1] = pack_bf16x2(x[2], x[3]) & live;
                     }
-                    return g;
-                };
 #pragma unroll
-                for (int m = 0; m < NBJ / 2; ++m) {
-                    const u32x4_t v = pack(value(2 * m), value(2 * m + 1));
-                    const int c = cl0 + 32 * m;
-                    const unsigned off =
-                        (r < R && c < Cc8) ? ((unsigned)r * (unsigned)ldc + (unsigned)c) * 2u : 0xFFFFFFF0u;
-                    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, (int)off, 0, 0);
+                    for (int m = 0; m < NBJ / 2; ++m) {
+                        const auto s0 = __builtin_amdgcn_permlane16_swap(w[2 * m][0], w[2 * m + 1][0], false, false);
+                        const auto s1 = __builtin_amdgcn_permlane16_swap(w[2 * m][1], w[2 * m + 1][1], false, false);
+                        const int c = cl0 + 32 * m;
+                        const unsigned off =
+                            (r < R && c < Cc8) ? ((unsigned)r * (unsigned)ldc + (unsigned)c) * 2u : 0xFFFFFFF0u;
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{s0[0], s1[0], s0[1], s1[1]}, rsrc, (int)off, 0,
+                                                               0);
+                    }
+                    if (!epi.GT) continue;
+                    // two rows of a column in a word: the even lane of two neighbours
+                    // takes their first column, the odd one their second.  The words of
+                    // a column's 32 rows are 64 bytes of the wave's LDS, their 16-byte
+                    // chunk c at c ^ (column / 4): at most two lanes on a bank
+#pragma unroll
+                    for (int j = 0; j < NBJ; ++j)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const unsigned other = __builtin_amdgcn_mov_dpp(w[j][u], 0xB1, 0xF, 0xF, true);
+                            const int c = 16 * j + 4 * lh + 2 * u + (lr & 1);
+                            turn[c * 16 + (((2 * ii + (lr >> 3)) ^ lh) << 2) + ((lr >> 1) & 3)] =
+                                __builtin_amdgcn_perm(other, w[j][u], pick);
+                        }
                 }
+                if (!epi.GT) continue;
+                __builtin_amdgcn_wave_barrier();  // the wave's own LDS, in order
+#pragma unroll
+                for (int q = 0; q < BN / 32; ++q) {
+                    const int c = 16 * q + (lane >> 2), n = row0 + 32 * h + 8 * (lane & 3);
+                    const u32x4_t v =
+                        *reinterpret_cast<const u32x4_t*>(turn + c * 16 + (((lane & 3) ^ ((c >> 2) & 3)) << 2));
+                    // rows of GT are padded to a multiple of 8
+                    if (n < R && col0 + c < Cc)
+                        *reinterpret_cast<u32x4_t*>(epi.GT + (int64_t)(col0 + c) * epi.ldgt + n) = v;
+                }
+                __builtin_amdgcn_wave_barrier();
             }
         } else {
             const float a = epi.last ? epi.scale[0] : 1.f;
@@ -264,9 +317,10 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
     constexpr int ST = LOSS ? 0 : C::NST;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM];
     __shared__ int pair_role;
-    // the sums of 16 rows of each wave, for entries at any column (MODE_STATS): all
-    // that the half-stages leave of the LDS
-    __shared__ __attribute__((aligned(16))) float spare[MODE == V3_STATS ? V3_NW * 16 * 128 : 1];
+    // all that the half-stages leave of the LDS, 8 KB a wave: the sums of 16 rows, for
+    // entries at any column (MODE_STATS), or 32 rows of G, for its transpose (MODE_GRAD)
+    constexpr bool SPARE = MODE == V3_STATS || MODE == V3_GRAD;
+    __shared__ __attribute__((aligned(16))) float spare[SPARE ? V3_NW * 16 * 128 : 1];
 
     const int ktiles = (D + V3_BK - 1) / V3_BK;
     const int kt0 = blockIdx.y * ktiles_per_split;
@@ -447,7 +501,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         // columns wcol0 + 16 j + 4 lh + {0..3}
         if constexpr (LOSS) {
             v3_loss_epilogue<MODE, BN>(acc, epi, Cout, ldc, row0 + wrow0, col0 + wcol0,
-                                       (tile_c * BN + wcol0) / (BN / 2), R, Cc, lane, spare + (MODE == V3_STATS ? wave * 16 * 128 : 0));
+                                       (tile_c * BN + wcol0) / (BN / 2), R, Cc, lane, spare + (SPARE ? wave * 16 * 128 : 0));
         } else {
         float* tpart = nullptr;
         unsigned long long* tstate = nullptr;

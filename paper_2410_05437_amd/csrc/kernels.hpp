@@ -120,6 +120,8 @@ struct LossEpi {
     int T = 0;
     const float* lse = nullptr;
     const float* r = nullptr;
+    uint16_t* GT = nullptr;                // C's transpose, if wanted (rows padded to 8 elements)
+    int64_t ldgt = 0;
     float* acc = nullptr;
     int64_t ldacc = 0;
     const float* scale = nullptr;

@@ -322,7 +322,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         espace::GradOut go;
         go.G = dX || fused ? G : nullptr;
         go.ldg = b.ldp;
-        go.GT = dW && !fused ? GT : nullptr;
+        go.GT = dW ? GT : nullptr;
         go.ldgt = ldgt;
         go.ldx = b.ldn;
         go.terms = b.terms;
@@ -334,6 +334,8 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             e.labels = t.labels;
             e.lse = lse;
             e.r = r;
+            e.GT = dW ? (uint16_t*)GT : nullptr;
+            e.ldgt = ldgt;
             ESPACE_TRY(run_tn_loss(X, ldx, Wp, ldw, G, b.ldp, N, cols, K, b.tile, espace::LOSS_GRAD, e, stream));
         } else {
             espace::Logits s;
@@ -344,8 +346,6 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         if (!t.labels)
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
                                                                        (int)cols, go, stream));
-        if (dW && fused)
-            ESPACE_LAUNCH("transpose", espace::launch_transpose(G, b.ldp, (int)N, (int)cols, GT, b.ldn, f32, stream));
         if (dX) {
             ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, b.ldp, f32, stream));
             if (ex.how == End::EPILOGUE) {
