@@ -186,7 +186,8 @@ def padded_empty(rows, cols, dtype, device, align=8):
     """Uninitialised rows x cols tensor with a leading dimension rounded up to
     `align` elements (its storage holds rows*ld elements)."""
     ld = max((cols + align - 1) // align * align, align)
-    return torch.empty((rows, ld), dtype=dtype, device=device)[:, :cols]
+    t = torch.empty((rows, ld), dtype=dtype, device=device)
+    return t if ld == cols else t[:, :cols]
 
 
 def _same(first, fname, *others):

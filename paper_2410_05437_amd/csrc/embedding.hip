@@ -39,10 +39,12 @@ __device__ __forceinline__ Piece<E> load_piece(const E* p) {
     return __builtin_bit_cast(Piece<E>, *reinterpret_cast<const u32x4_t*>(p));
 }
 // the elements of columns below C, of the W from column c on
-template <typename E>
+template <typename E, bool STREAM = false>
 __device__ __forceinline__ void store_piece(E* row, int64_t c, int64_t C, const Piece<E>& v) {
     if (c + Piece<E>::W <= C) {
-        *reinterpret_cast<u32x4_t*>(row + c) = __builtin_bit_cast(u32x4_t, v);
+        u32x4_t* p = reinterpret_cast<u32x4_t*>(row + c);
+        if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), p);
+        else *p = __builtin_bit_cast(u32x4_t, v);
     } else {
 #pragma unroll
         for (int e = 0; e < Piece<E>::W; ++e)
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(256) void reduce_runs_kernel(const int64_t* __restr
         for (int e = 0; e < W; ++e) z.v[e] = to_elem(0.f, E());
         if (c < K)
             for (int k = group; k < RUN_MOST; k += groups)
-                if ((empty >> k) & 1) store_piece(dE + (int64_t)(v0 + k) * ldde, c, K, z);
+                if ((empty >> k) & 1) store_piece<E, true>(dE + (int64_t)(v0 + k) * ldde, c, K, z);
         return;
     }
     // rows of the workgroup's places, and the entries of those and their neighbours

@@ -170,16 +170,35 @@ __device__ __forceinline__ f32x4_t logits4(const float* p, const Logits& S) {
     return x;
 }
 
+// A token's loss from its targets' logits; all lanes of a wave, for an entry each.
+__device__ __forceinline__ float entries_loss(const LossTargets& t, int64_t row, int lane, float ls,
+                                              float* __restrict__ picked, float tt) {
+    float v = 0.f;
+    for (int j = lane; j < t.T; j += 64) {
+        const int64_t at = row * t.T + j;
+        if (t.col[at] < 0) picked[j] = 0.f;
+        else if (t.p[at] != 0.f) v += t.p[at] * ((t.logp[at] + ls) - picked[j]);
+    }
+    return wave_sum(v) * tt;
+}
+__device__ __forceinline__ float label_loss(int64_t label, int V, float ls, float logit) {
+    return label >= V ? nan_f() : (label >= 0 ? ls - logit : 0.f);
+}
+
 // STAT_COLS columns of one token: 256 threads of 4 x 4 columns each, kept in
-// registers between the maximum and the sum.
+// registers between the maximum and the sum.  WHOLE: they are all of the vocabulary,
+// and the token's loss follows at once.
+template <bool WHOLE>
 __global__ __launch_bounds__(256) void stats_kernel(Logits S, int c0, int cols,
                                                     float inv_t, LossTargets t, float2* __restrict__ part, int N,
-                                                    int part0, int n0, float* __restrict__ picked, int64_t ldpk) {
+                                                    int part0, int n0, float* __restrict__ picked, int64_t ldpk,
+                                                    float tt, float* __restrict__ loss, float* __restrict__ lse) {
     __shared__ float red[8];
     const int n = n0 + blockIdx.y;
     const int b0 = blockIdx.x * STAT_COLS;
     const int left = cols - b0 < STAT_COLS ? cols - b0 : STAT_COLS;
     const float* row = S.S + (int64_t)n * S.lds + b0;
+    float* pick = picked + (int64_t)n * ldpk;
     float v[4][4];
     float m = -INFINITY;
 #pragma unroll
@@ -192,6 +211,14 @@ __global__ __launch_bounds__(256) void stats_kernel(Logits S, int c0, int cols,
         for (int e = 0; e < 4; ++e) {
             v[i][e] = c + e < left ? x[e] * inv_t : -INFINITY;
             m = fmaxf(m, v[i][e]);
+        }
+    }
+    for (int j = threadIdx.x; j < t.T; j += 256) {
+        const int64_t c = (t.labels ? t.labels[n] : (int64_t)t.col[(int64_t)n * t.T + j]) - c0 - b0;
+        if (c >= 0 && c < left) {
+            float x = row[c];
+            for (int s = 1; s < S.slabs; ++s) x += row[c + s * S.stride];
+            pick[j] = x * inv_t;
         }
     }
     m = wave_max(m);
@@ -208,18 +235,19 @@ __global__ __launch_bounds__(256) void stats_kernel(Logits S, int c0, int cols,
         for (int e = 0; e < 4; ++e) l += exp_f(v[i][e] - base);
     l = wave_sum(l);
     if (lane == 0) red[4 + wave] = l;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        l = (red[4] + red[5]) + (red[6] + red[7]);
-        part[(int64_t)(part0 + blockIdx.x) * N + n] = make_float2(l == 0.f ? -INFINITY : base, l);
+    __syncthreads();                              // and the logits at `pick` are written
+    if (wave != 0) return;
+    l = (red[4] + red[5]) + (red[6] + red[7]);
+    if constexpr (!WHOLE) {
+        if (lane == 0) part[(int64_t)(part0 + blockIdx.x) * N + n] = make_float2(l == 0.f ? -INFINITY : base, l);
+        return;
     }
-    for (int j = threadIdx.x; j < t.T; j += 256) {
-        const int64_t c = (t.labels ? t.labels[n] : (int64_t)t.col[(int64_t)n * t.T + j]) - c0 - b0;
-        if (c >= 0 && c < left) {
-            float x = row[c];
-            for (int s = 1; s < S.slabs; ++s) x += row[c + s * S.stride];
-            picked[(int64_t)n * ldpk + j] = x * inv_t;
-        }
+    const float ls = m == -INFINITY && l == 0.f ? -INFINITY : base + logf(l);
+    const float x = t.labels ? (lane == 0 ? label_loss(t.labels[n], cols, ls, pick[0]) : 0.f)
+                             : entries_loss(t, n, lane, ls, pick, tt);
+    if (lane == 0) {
+        loss[n] = x;
+        lse[n] = ls;
     }
 }
 
@@ -253,10 +281,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ 
         lse_of[x] = ls;
         if (n < N) {
             lse[n] = ls;
-            if (t.labels) {
-                const int64_t c = t.labels[n];
-                loss[n] = c >= V ? nan_f() : (c >= 0 ? ls - picked[(int64_t)n * ldpk] : 0.f);
-            }
+            if (t.labels) loss[n] = label_loss(t.labels[n], V, ls, picked[(int64_t)n * ldpk]);
         }
     }
     if (t.labels) return;
@@ -264,17 +289,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int k = wave; k < 16 && (int)blockIdx.x * 16 + k < N; k += 4) {
         const int64_t row = (int64_t)blockIdx.x * 16 + k;
-        const float ls = lse_of[k];
-        float v = 0.f;
-        for (int j = lane; j < t.T; j += 64) {
-            const int64_t at = row * t.T + j;
-            if (t.col[at] < 0) {
-                picked[row * ldpk + j] = 0.f;
-            } else if (t.p[at] != 0.f) {
-                v += t.p[at] * ((t.logp[at] + ls) - picked[row * ldpk + j]);
-            }
-        }
-        v = wave_sum(v) * tt;
+        const float v = entries_loss(t, row, lane, lse_of[k], picked + row * ldpk, tt);
         if (lane == 0) loss[row] = v;
     }
 }
@@ -319,12 +334,24 @@ __device__ __forceinline__ float zero_of(float) { return 0.f; }
 template <typename E>
 __global__ __launch_bounds__(256) void grad_kernel(Logits S, int N, int c0, int cols,
                                                    float inv_t, const float* __restrict__ lse,
-                                                   const float* __restrict__ r, const int64_t* __restrict__ labels,
+                                                   const float* __restrict__ r, LossTargets t, int entries,
                                                    GradOut out) {
+    __shared__ float less[64][65];                // Σ p of the tile's entries
     __shared__ E tile[64][64 + 4 / sizeof(E)];
     const int n0 = blockIdx.y * 64, b0 = blockIdx.x * 64;
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4;    // 4 columns, 16 rows a pass
     float g[4][4];
+    if (entries) {
+        for (int i = threadIdx.x; i < 64 * 64; i += 256) less[i >> 6][i & 63] = 0.f;
+        __syncthreads();
+        // (an entry has one place after its equals were added to it)
+        const int64_t end = min((int64_t)N, (int64_t)n0 + 64) * t.T;
+        for (int64_t at = (int64_t)n0 * t.T + threadIdx.x; at < end; at += 256) {
+            const int c = t.col[at] - c0 - b0;
+            if (t.col[at] >= 0 && c >= 0 && c < 64) less[at / t.T - n0][c] = t.p[at];
+        }
+        __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int n = n0 + i * 16 + y, c = b0 + 4 * x;
@@ -334,11 +361,12 @@ __global__ __launch_bounds__(256) void grad_kernel(Logits S, int N, int c0, int 
         const float rn = r[n];
         const f32x4_t s = logits4(S.S + (int64_t)n * S.lds + c, S);
         const float ls = lse[n];
-        const int64_t at = labels ? labels[n] - c0 - c : -1;
+        const int64_t at = t.labels ? t.labels[n] - c0 - c : -1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float v = exp_f(s[e] * inv_t - ls);
             if (at == e) v -= 1.f;
+            if (entries) v -= less[i * 16 + y][4 * x + e];
             // a token without a target: 0 whatever its logits are
             g[i][e] = rn == 0.f ? 0.f : rn * v;
         }
@@ -501,8 +529,18 @@ hipError_t launch_loss_stats(const Logits& S, int N, int c0, int cols, float inv
     const int chunks = (cols + STAT_COLS - 1) / STAT_COLS;
     for (int n0 = 0; n0 < N; n0 += 65535) {
         const int rows = N - n0 < 65535 ? N - n0 : 65535;
-        hipLaunchKernelGGL(stats_kernel, dim3(chunks, rows), dim3(256), 0, stream, S, c0, cols, inv_t, t, part, N,
-                           part0, n0, picked, ldpk);
+        hipLaunchKernelGGL(stats_kernel<false>, dim3(chunks, rows), dim3(256), 0, stream, S, c0, cols, inv_t, t, part, N,
+                           part0, n0, picked, ldpk, 0.f, nullptr, nullptr);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_whole(const Logits& S, int N, int V, float temperature, const LossTargets& t, float* picked,
+                             int64_t ldpk, float* loss, float* lse, hipStream_t stream) {
+    for (int n0 = 0; n0 < N; n0 += 65535) {
+        const int rows = N - n0 < 65535 ? N - n0 : 65535;
+        hipLaunchKernelGGL(stats_kernel<true>, dim3(1, rows), dim3(256), 0, stream, S, 0, V, 1.f / temperature, t, nullptr,
+                           N, 0, n0, picked, ldpk, temperature * temperature, loss, lse);
     }
     return hipGetLastError();
 }
@@ -524,13 +562,15 @@ hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const flo
 static_assert((1 << 22) / 64 <= 65536, "launch limit");
 
 hipError_t launch_loss_grad(const Logits& S, int N, int c0, int cols, float inv_t, const float* lse,
-                            const float* r, const int64_t* labels, const GradOut& out, hipStream_t stream) {
+                            const float* r, const LossTargets& t, bool entries, const GradOut& out,
+                            hipStream_t stream) {
     const dim3 grid((cols + 63) / 64, (N + 63) / 64), block(256);
     if (out.f32)
-        hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S, N, c0, cols, inv_t, lse, r, labels, out);
+        hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, S, N, c0, cols, inv_t, lse, r, t,
+                           entries ? 1 : 0, out);
     else
-        hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S, N, c0, cols, inv_t, lse, r, labels,
-                           out);
+        hipLaunchKernelGGL(grad_kernel<uint16_t>, grid, block, 0, stream, S, N, c0, cols, inv_t, lse, r, t,
+                           entries ? 1 : 0, out);
     return hipGetLastError();
 }
 

@@ -56,6 +56,10 @@ struct Logits {
 hipError_t launch_loss_stats(const Logits& S, int N, int c0, int cols, float inv_t,
                              const LossTargets& t, float2* part, int part0, float* picked, int64_t ldpk,
                              hipStream_t stream);
+// The whole vocabulary's (V <= STAT_COLS): loss and lse, and picked with its empty
+// places.
+hipError_t launch_loss_whole(const Logits& S, int N, int V, float temperature, const LossTargets& t, float* picked,
+                             int64_t ldpk, float* loss, float* lse, hipStream_t stream);
 // loss and lse from the nparts parts of each token; picked of empty places.
 hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, float temperature, const LossTargets& t,
                               float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream);
@@ -76,10 +80,11 @@ struct GradOut {
     int terms = 1;
     bool f32 = false;
 };
-// G of columns [c0, c0 + cols) from their logits; labels may be NULL (their entries are
-// launch_loss_fix's).
+// G of columns [c0, c0 + cols) from their logits; entries: with those of a teacher,
+// else they are launch_loss_fix's.
 hipError_t launch_loss_grad(const Logits& S, int N, int c0, int cols, float inv_t, const float* lse,
-                            const float* r, const int64_t* labels, const GradOut& out, hipStream_t stream);
+                            const float* r, const LossTargets& t, bool entries, const GradOut& out,
+                            hipStream_t stream);
 // The teacher's entries among these columns, from their logits `picked`.
 hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ldpk, const float* lse, const float* r,
                            int N, int c0, int cols, const GradOut& out, hipStream_t stream);

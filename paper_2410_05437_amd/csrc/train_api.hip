@@ -35,8 +35,10 @@ int64_t piece_cols(int64_t N, int64_t V, int64_t elems) {
 }
 
 // Pieces that are kept as float32 logits: 128 MB, half the Infinity Cache.  Those of G
-// where the logits stay in registers (bfloat16; G and its transpose): the same.
-constexpr int64_t kLogits = (int64_t)1 << 25, kGrads = (int64_t)1 << 25;
+// where the logits stay in registers: as much, and as much again its transpose (twice
+// that of half as wide pieces: 8192 tokens on 50257 x 6144 16.7 -> 15.9 ms, with fewer
+// passes over dX's sums; 4096 on 32000 x 4096 3.46 -> 3.50).
+constexpr int64_t kLogits = (int64_t)1 << 25, kGrads = (int64_t)1 << 26;
 // Where the epilogues cannot take a call's leading dimensions: narrow pieces, which fit
 // any layout.
 constexpr int64_t kNarrow = 256;
@@ -276,6 +278,11 @@ espace_status loss_forward(const void* X, int64_t ldx, const void* W, int64_t ld
             const int64_t cols = std::min(P, V - c0);
             espace::Logits s;
             ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, b.ranges_s, &s, stream));
+            if (cols == V && V <= espace::STAT_COLS) {
+                ESPACE_LAUNCH("loss", espace::launch_loss_whole(s, (int)N, (int)V, temperature, t, picked, ldpk, loss,
+                                                                lse, stream));
+                return ESPACE_OK;
+            }
             ESPACE_LAUNCH("loss statistics", espace::launch_loss_stats(s, (int)N, (int)c0, (int)cols, inv_t, t, part,
                                                                        parts, picked, ldpk, stream));
             parts += (int)((cols + espace::STAT_COLS - 1) / espace::STAT_COLS);
@@ -308,6 +315,9 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     const int64_t rows = N * b.terms, slab = rows * b.ldk;      // of dX's sums
     const bool many = pieces <= 4 && !narrow;                   // their ranges stay apart
     const int64_t ldgt = b.ldn * b.terms;
+    // up to as many entries as a tile of G has columns: with the tile (its 64 tokens'
+    // entries are looked through for each), else by a pass over the entries
+    const bool few = !t.labels && !fused && t.T <= 64;
     int sums = 0;                                               // slabs in acc
     log_plan(b, true, fused, N, K, V, t.labels ? 0 : t.T, P);
     ESPACE_LAUNCH("loss coefficients", espace::launch_loss_coef(dloss, t.labels, mass, temperature, (int)N, (int)V, r,
@@ -340,10 +350,10 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         } else {
             espace::Logits s;
             ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, b.ranges_s, &s, stream));
-            ESPACE_LAUNCH("logits' gradient", espace::launch_loss_grad(s, (int)N, (int)c0, (int)cols, inv_t, lse, r,
-                                                                       t.labels, go, stream));
+            ESPACE_LAUNCH("logits' gradient", espace::launch_loss_grad(s, (int)N, (int)c0, (int)cols, inv_t, lse, r, t,
+                                                                       few, go, stream));
         }
-        if (!t.labels)
+        if (!t.labels && !few)
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
                                                                        (int)cols, go, stream));
         if (dX) {
