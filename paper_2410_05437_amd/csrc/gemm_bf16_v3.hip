@@ -38,6 +38,10 @@ namespace {
 
 struct V3NoEpi {};
 
+// B as [Cc][D] (rows along the depth), or as [D][Cc]; SWAPPED: the latter, and C is
+// written transposed, [Cc][R].
+enum { V3_B_ROWS = 0, V3_B_DEPTH = 1, V3_B_SWAPPED = 2 };
+
 // f over the four lanes that share a row (16 apart); every one gets the result
 template <class F>
 __device__ __forceinline__ float v3_over_row(float x, F f) {
@@ -51,7 +55,9 @@ __device__ __forceinline__ float v3_over_row(float x, F f) {
 // The rows of a wave's 128 x BN/2 sub-tile are spread as elsewhere: block (i, j), row
 // 16 i + lane % 16, columns 16 j + 4 (lane / 16) + {0..3}.  row0, col0: the sub-tile's
 // first row and column; slab: its index among the slabs of BN/2 columns.
-template <int MODE, int BN, class EPI>
+// SWAP (MODE_GRAD_OUT, last, nothing to add): C is [Cc][R]; a lane holds column 16 j +
+// lane % 16 of block (i, j) and rows 16 i + 4 (lane / 16) + {0..3}.
+template <int MODE, int BN, bool SWAP, class EPI>
 __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3Cfg<BN>::NBJ], const EPI& epi,
                                                  void* Cout, int64_t ldc, int row0, int col0, int slab, int R, int Cc,
                                                  int lane, float* spare) {
@@ -240,6 +246,27 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
                 }
                 __builtin_amdgcn_wave_barrier();
             }
+        } else if constexpr (SWAP) {
+            const float a = epi.scale[0];
+            const int r8 = row0 + 16 * (lh & 1) + 8 * (lh >> 1);   // + 32 m
+#pragma unroll
+            for (int j = 0; j < NBJ; ++j) {
+                const int c = col0 + 16 * j + lr;
+#pragma unroll
+                for (int m = 0; m < V3_NB / 2; ++m) {
+                    const u32x4_t v = pack(v3_acc_read(acc[2 * m][j]) * a, v3_acc_read(acc[2 * m + 1][j]) * a);
+                    const int r = r8 + 32 * m;
+                    if (c >= Cc) continue;
+                    uint16_t* p = Cb + (int64_t)c * ldc + r;
+                    if (r + 8 <= R) {
+                        *reinterpret_cast<u32x4_t*>(p) = v;
+                    } else if (r < R) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (r + e < R) p[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                    }
+                }
+            }
         } else {
             const float a = epi.last ? epi.scale[0] : 1.f;
 #pragma unroll
@@ -303,7 +330,7 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
 // persistent like MODE_BF16.  Their epilogues read what belongs to the tile's rows,
 // so the wait for the next item's first step does not count on stores behind it
 // (ST = 0) and may wait for them as well.
-template <int MODE, int BN, int APAIR = 0, class EPI = V3NoEpi>
+template <int MODE, int BN, int APAIR = 0, class EPI = V3NoEpi, int BT = V3_B_ROWS>
 __global__ __launch_bounds__(256, 1)
 void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
                             const uint16_t* __restrict__ B, int64_t ldb,
@@ -339,7 +366,10 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
     const int wrow0 = (wave >> 1) * V3_WT;
     const int wcol0 = (wave & 1) * (BN / 2);
     const unsigned ra = (unsigned)((uint64_t)(APAIR ? (R + 1) / 2 : R) * lda * 2u);
-    const unsigned rb = (unsigned)((uint64_t)Cc * ldb * 2u);
+    constexpr bool T = BT != V3_B_ROWS, SWAP = BT == V3_B_SWAPPED;
+    const unsigned ldb2 = (unsigned)ldb * 2u;
+    const unsigned rb = T ? (unsigned)(((uint64_t)(D - 1) * ldb + ((Cc + 7) & ~7)) * 2u)
+                          : (unsigned)((uint64_t)Cc * ldb * 2u);
 
     // fragment row addresses: a lane reads row lane % 16 of each 16-row block
     // and depth chunk lane / 16 of the sub-step
@@ -349,7 +379,14 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
     const unsigned slot = (unsigned)((lh ^ v3_swz(lr)) * 16);
     const unsigned arow = sbase + (unsigned)((wrow0 + lr) * V3_ROWB) + slot;
-    const unsigned brow = sbase + (unsigned)((V3_BM + wcol0 + lr) * V3_ROWB) + slot;
+    // depth-major B: the lane's depth row 8 lh + lr / 4, 8 bytes lr % 4 of each 16-column
+    // block, whose places in the row are turn[]
+    const int trow = 8 * lh + (lr >> 2);
+    const unsigned brow = T ? sbase + (unsigned)(V3_BM * V3_ROWB + trow * BN * 2 + (lr & 3) * 8)
+                            : sbase + (unsigned)((V3_BM + wcol0 + lr) * V3_ROWB) + slot;
+    int turn[NBJ];
+#pragma unroll
+    for (int j = 0; j < NBJ; ++j) turn[j] = T ? ((wcol0 / 16 + j) ^ v3_turn<C>(trow)) * 32 : 0;
 
     f32x4_t acc[V3_NB][NBJ];
     bf16x8_t fa0[V3_NB], fb0[NBJ], fa1[V3_NB], fb1[NBJ];
@@ -383,12 +420,12 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         } else {
             // the half-stages may still be read by a wave finishing the previous item
             if (item != (int)blockIdx.x) __syncthreads();
-            v3_offsets<C, 1, APAIR != 0>(voff, row0, col0, R, Cc, lda, ldb, wave, lane);
-            int later = v3_load_half<C, APAIR != 0>(smem, A, B, ra, rb, voff, wave, lane, order(kt0), 0, hs(0, 0), D);
-            later = v3_load_half<C, APAIR != 0>(smem, A, B, ra, rb, voff, wave, lane, order(kt0), 1, hs(0, 1), D);
+            v3_offsets<C, 1, APAIR != 0, T>(voff, row0, col0, R, Cc, lda, ldb, wave, lane);
+            int later = v3_load_half<C, APAIR != 0, T>(smem, A, B, ra, rb, voff, wave, lane, order(kt0), 0, hs(0, 0), D, ldb2);
+            later = v3_load_half<C, APAIR != 0, T>(smem, A, B, ra, rb, voff, wave, lane, order(kt0), 1, hs(0, 1), D, ldb2);
             if (nsteps > 1) {
-                later = v3_load_half<C, APAIR != 0>(smem, A, B, ra, rb, voff, wave, lane, order(kt0 + 1), 0, hs(1, 0), D);
-                later += v3_load_half<C, APAIR != 0>(smem, A, B, ra, rb, voff, wave, lane, order(kt0 + 1), 1, hs(1, 1), D);
+                later = v3_load_half<C, APAIR != 0, T>(smem, A, B, ra, rb, voff, wave, lane, order(kt0 + 1), 0, hs(1, 0), D, ldb2);
+                later += v3_load_half<C, APAIR != 0, T>(smem, A, B, ra, rb, voff, wave, lane, order(kt0 + 1), 1, hs(1, 1), D, ldb2);
             } else {
                 later = 0;
             }
@@ -399,7 +436,10 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         }
         __builtin_amdgcn_s_barrier();
 #pragma unroll
-        for (int x = 0; x < C::NRD; ++x) v3_read_dyn<NBJ>(x, fa0, fb0, aA0, aB0);
+        for (int x = 0; x < C::NRD; ++x) {
+            if constexpr (T) v3_read_bt<C>(x, fa0, fb0, aA0, aB0, turn);
+            else v3_read_dyn<NBJ>(x, fa0, fb0, aA0, aB0);
+        }
         v3_wait_lgkm0();
         // the first sub-step loads step kt0 + 2 into the half-stage just read:
         // every wave's reads of it must be complete before any wave issues them
@@ -420,7 +460,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
             lkt = order(kt0 + (kt + 2 - kt_end));
             if (!ahead_next) return 0;
             if (kt + 2 == kt_end && h == 0)
-                v3_offsets<C, 1, APAIR != 0>(voff, ntr * V3_BM, ntc * BN, R, Cc, lda, ldb, wave, lane);
+                v3_offsets<C, 1, APAIR != 0, T>(voff, ntr * V3_BM, ntc * BN, R, Cc, lda, ldb, wave, lane);
             return 1;
         };
         // one step with the stage chosen at run time (the first one and the
@@ -433,9 +473,9 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
             // sub-step 0: fragments of sub-step 1 from the second half-stage
             int lkt;
             const int k0 = load_kind(0, lkt);
-            v3_substep<C, F, true, true, APAIR != 0>(acc, fa0, fb0, fa1, fb1, rel ? aA3 : aA1, rel ? aB3 : aB1, smem,
-                                         A, B, ra, rb, voff, wave, lkt, 0, hs(rel, 0), k0 == 1);
-            if (k0 == 2) v3_load_half<C, APAIR != 0>(smem, A, B, ra, rb, voff, wave, lane, lkt, 0, hs(rel, 0), D);
+            v3_substep<C, F, true, true, APAIR != 0, T, SWAP>(acc, fa0, fb0, fa1, fb1, rel ? aA3 : aA1, rel ? aB3 : aB1, smem,
+                                         A, B, ra, rb, voff, wave, lkt, 0, hs(rel, 0), k0 == 1, ldb2, turn);
+            if (k0 == 2) v3_load_half<C, APAIR != 0, T>(smem, A, B, ra, rb, voff, wave, lane, lkt, 0, hs(rel, 0), D, ldb2);
             const int n0 = k0 == 1 ? C::LPH : 0;
             v3_wait_lgkm0();
             if (kt + 1 < kt_end || ahead_next) {
@@ -447,9 +487,9 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
             // last step the reads are of no use but harmless: one code path
             // keeps the accumulators in place)
             const int k1 = load_kind(1, lkt);
-            v3_substep<C, false, true, true, APAIR != 0>(acc, fa1, fb1, fa0, fb0, rel ? aA0 : aA2, rel ? aB0 : aB2,
-                                             smem, A, B, ra, rb, voff, wave, lkt, 1, hs(rel, 1), k1 == 1);
-            if (k1 == 2) v3_load_half<C, APAIR != 0>(smem, A, B, ra, rb, voff, wave, lane, lkt, 1, hs(rel, 1), D);
+            v3_substep<C, false, true, true, APAIR != 0, T, SWAP>(acc, fa1, fb1, fa0, fb0, rel ? aA0 : aA2, rel ? aB0 : aB2,
+                                             smem, A, B, ra, rb, voff, wave, lkt, 1, hs(rel, 1), k1 == 1, ldb2, turn);
+            if (k1 == 2) v3_load_half<C, APAIR != 0, T>(smem, A, B, ra, rb, voff, wave, lane, lkt, 1, hs(rel, 1), D, ldb2);
             const int n1 = k1 == 1 ? C::LPH : 0;
             v3_wait_lgkm0();
             if (kt + 1 < kt_end) {
@@ -466,23 +506,23 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         // barrier waits for the half-stage the next sub-step reads, with the
         // two newer half-steps of loads in flight
         while (kt + 3 < nfull) {
-            v3_substep<C, false, true, true, APAIR != 0>(acc, fa0, fb0, fa1, fb1, aA3, aB3, smem, A, B, ra, rb, voff,
-                                             wave, order(kt + 2), 0, hs(1, 0));
+            v3_substep<C, false, true, true, APAIR != 0, T, SWAP>(acc, fa0, fb0, fa1, fb1, aA3, aB3, smem, A, B, ra, rb, voff,
+                                             wave, order(kt + 2), 0, hs(1, 0), true, ldb2, turn);
             v3_wait_lgkm0();
             v3_wait_vm<2 * C::LPH>();
             __builtin_amdgcn_s_barrier();
-            v3_substep<C, false, true, true, APAIR != 0>(acc, fa1, fb1, fa0, fb0, aA0, aB0, smem, A, B, ra, rb, voff,
-                                             wave, order(kt + 2), 1, hs(1, 1));
+            v3_substep<C, false, true, true, APAIR != 0, T, SWAP>(acc, fa1, fb1, fa0, fb0, aA0, aB0, smem, A, B, ra, rb, voff,
+                                             wave, order(kt + 2), 1, hs(1, 1), true, ldb2, turn);
             v3_wait_lgkm0();
             v3_wait_vm<2 * C::LPH>();
             __builtin_amdgcn_s_barrier();
-            v3_substep<C, false, true, true, APAIR != 0>(acc, fa0, fb0, fa1, fb1, aA1, aB1, smem, A, B, ra, rb, voff,
-                                             wave, order(kt + 3), 0, hs(0, 0));
+            v3_substep<C, false, true, true, APAIR != 0, T, SWAP>(acc, fa0, fb0, fa1, fb1, aA1, aB1, smem, A, B, ra, rb, voff,
+                                             wave, order(kt + 3), 0, hs(0, 0), true, ldb2, turn);
             v3_wait_lgkm0();
             v3_wait_vm<2 * C::LPH>();
             __builtin_amdgcn_s_barrier();
-            v3_substep<C, false, true, true, APAIR != 0>(acc, fa1, fb1, fa0, fb0, aA2, aB2, smem, A, B, ra, rb, voff,
-                                             wave, order(kt + 3), 1, hs(0, 1));
+            v3_substep<C, false, true, true, APAIR != 0, T, SWAP>(acc, fa1, fb1, fa0, fb0, aA2, aB2, smem, A, B, ra, rb, voff,
+                                             wave, order(kt + 3), 1, hs(0, 1), true, ldb2, turn);
             v3_wait_lgkm0();
             v3_wait_vm<2 * C::LPH>();
             __builtin_amdgcn_s_barrier();
@@ -500,7 +540,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         // block (i, j): lane holds output row wrow0 + 16 i + lr and the 4
         // columns wcol0 + 16 j + 4 lh + {0..3}
         if constexpr (LOSS) {
-            v3_loss_epilogue<MODE, BN>(acc, epi, Cout, ldc, row0 + wrow0, col0 + wcol0,
+            v3_loss_epilogue<MODE, BN, SWAP>(acc, epi, Cout, ldc, row0 + wrow0, col0 + wcol0,
                                        (tile_c * BN + wcol0) / (BN / 2), R, Cc, lane, spare + (SPARE ? wave * 16 * 128 : 0));
         } else {
         float* tpart = nullptr;
@@ -700,9 +740,14 @@ hipError_t launch_v3_ranges(const GemmArgs& g, bool upper, int* ranges, hipStrea
     const int S = (ktiles + ktps - 1) / ktps;
     *ranges = S;
     const int64_t ldp = splitk_ld(g.Cc);
-    hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN>), dim3(ntiles, S), dim3(V3_NW * 64), 0, stream, g.A,
-                       g.lda, g.B, g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D, tiles_c, ntiles, ktps,
-                       (int64_t)g.R * ldp, upper ? 8 : 0, nullptr, nullptr, 0ull, g.wait, 0, V3NoEpi{});
+    if (g.b_depth)
+        hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN, 0, V3NoEpi, V3_B_DEPTH>), dim3(ntiles, S),
+                           dim3(V3_NW * 64), 0, stream, g.A, g.lda, g.B, g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D,
+                           tiles_c, ntiles, ktps, (int64_t)g.R * ldp, 0, nullptr, nullptr, 0ull, g.wait, 0, V3NoEpi{});
+    else
+        hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN>), dim3(ntiles, S), dim3(V3_NW * 64), 0, stream, g.A,
+                           g.lda, g.B, g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D, tiles_c, ntiles, ktps,
+                           (int64_t)g.R * ldp, upper ? 8 : 0, nullptr, nullptr, 0ull, g.wait, 0, V3NoEpi{});
     return hipGetLastError();
 }
 
@@ -716,14 +761,15 @@ static hipError_t launch_loss(const GemmArgs& g, LossMode mode, const LossEpi& e
     const int persistent = g.cus > 0 ? g.cus : 256;
     const dim3 grid(ntiles < persistent ? ntiles : persistent, 1), block(V3_NW * 64);
     const int map = one_depth_order(g, V3_BM, BN) ? MAP_ONE_ORDER : 0;
-#define LAUNCH(MODE)                                                                                                  \
-    hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<MODE, BN, 0, LossEpi>), grid, block, 0, stream, g.A, g.lda, g.B, g.ldb, \
+#define LAUNCH(MODE, BT)                                                                                              \
+    hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<MODE, BN, 0, LossEpi, BT>), grid, block, 0, stream, g.A, g.lda, g.B, g.ldb, \
                        g.C, g.ldc, g.R, g.Cc, g.D, tiles_c, ntiles, ktiles, (int64_t)0, map, nullptr, nullptr, 0ull,  \
                        g.wait, 0, epi)
     switch (mode) {
-        case LOSS_STATS: LAUNCH(V3_STATS); break;
-        case LOSS_GRAD: LAUNCH(V3_GRAD); break;
-        case LOSS_GRAD_OUT: LAUNCH(V3_GRAD_OUT); break;
+        case LOSS_STATS: LAUNCH(V3_STATS, V3_B_ROWS); break;
+        case LOSS_GRAD: LAUNCH(V3_GRAD, V3_B_ROWS); break;
+        case LOSS_GRAD_OUT: LAUNCH(V3_GRAD_OUT, V3_B_DEPTH); break;
+        case LOSS_GRAD_OUT_T: LAUNCH(V3_GRAD_OUT, V3_B_SWAPPED); break;
     }
 #undef LAUNCH
     return hipGetLastError();
@@ -731,8 +777,10 @@ static hipError_t launch_loss(const GemmArgs& g, LossMode mode, const LossEpi& e
 
 hipError_t launch_gemm_tn_bf16_loss(const GemmArgs& g, LossMode mode, const LossEpi& epi, hipStream_t stream) {
     const int64_t lim = (int64_t)1 << 31;
-    if ((int64_t)g.R * g.lda >= lim || (int64_t)g.Cc * g.ldb >= lim || g.D < 1 ||
-        (mode == LOSS_GRAD && (int64_t)g.R * g.ldc >= lim))
+    const bool depth = mode == LOSS_GRAD_OUT || mode == LOSS_GRAD_OUT_T;
+    if ((int64_t)g.R * g.lda >= lim || (int64_t)(depth ? g.D : g.Cc) * g.ldb >= lim || g.D < 1 ||
+        (mode == LOSS_GRAD && (int64_t)g.R * g.ldc >= lim) ||
+        (mode == LOSS_GRAD_OUT_T && (epi.add || !epi.last)))
         return hipErrorInvalidValue;
     switch (g.tile) {
         case TILE_256x256: return launch_loss<256>(g, mode, epi, stream);
@@ -743,9 +791,9 @@ hipError_t launch_gemm_tn_bf16_loss(const GemmArgs& g, LossMode mode, const Loss
 
 hipError_t launch_gemm_tn_bf16_v3_ranges(const GemmArgs& g, bool upper, int* ranges, hipStream_t stream) {
     const int64_t lim = (int64_t)1 << 31;
-    if ((int64_t)g.R * g.lda >= lim || (int64_t)g.Cc * g.ldb >= lim || g.D < 1 || !g.partial)
+    if ((int64_t)g.R * g.lda >= lim || (int64_t)(g.b_depth ? g.D : g.Cc) * g.ldb >= lim || g.D < 1 || !g.partial)
         return hipErrorInvalidValue;
-    if (upper && g.R != g.Cc) return hipErrorInvalidValue;
+    if (upper && (g.b_depth || g.R != g.Cc)) return hipErrorInvalidValue;
     switch (g.tile) {
         case TILE_256x256: return launch_v3_ranges<256>(g, upper, ranges, stream);
         case TILE_256x192: return launch_v3_ranges<192>(g, upper, ranges, stream);

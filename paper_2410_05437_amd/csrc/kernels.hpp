@@ -50,6 +50,7 @@ struct GemmArgs {
     // one whole cache line.  ld (elements per row pair) is a multiple of 64.
     int a_pairs = 0;    // A is in the row-pair layout (lda its pair pitch)
     int c_pairs = 0;    // write C (bf16) in the row-pair layout (ldc its pair pitch)
+    int b_depth = 0;    // B is [D][Cc] (depth ranges of the four-wave kernel)
     const float* scale = nullptr;   // small tiles in one range: C = scale[0] * sums, rounded
 };
 
@@ -102,8 +103,9 @@ hipError_t launch_gemm_tn_bf16_v4(const GemmArgs& g, hipStream_t stream);
 //            for the k-th such slab, and s·inv_t of the targets
 //  grad      C = r[row]·(exp(s·inv_t - lse[row]) - [column = labels[row]]) in bfloat16,
 //            0 where r is 0, zeros up to a multiple of 8 columns
-//  grad_out  a gradient: acc (if add) + s is stored in acc, or times scale[0] in C
-//            in bfloat16 (if last)
+//  grad_out  a gradient, with B as [D][Cc]: acc (if add) + s is stored in acc, or times
+//            scale[0] in C in bfloat16 (if last)
+//  grad_out_t  the same, last and not added to anything, C written as [Cc][R]
 struct LossEpi {
     float inv_t = 1.f;
     int col0 = 0;
@@ -127,7 +129,7 @@ struct LossEpi {
     const float* scale = nullptr;
     int add = 0, last = 0;
 };
-enum LossMode { LOSS_STATS, LOSS_GRAD, LOSS_GRAD_OUT };
+enum LossMode { LOSS_STATS, LOSS_GRAD, LOSS_GRAD_OUT, LOSS_GRAD_OUT_T };
 // 256 x 256 and 256 x 192 plans (g.tile) with these epilogues; loss_slab: the columns
 // of a slab of the tile.  hipErrorInvalidValue for matrices of 2^31 elements or more.
 inline int loss_slab(int tile) { return tile == TILE_256x192 ? 96 : 128; }

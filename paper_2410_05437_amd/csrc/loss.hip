@@ -380,7 +380,8 @@ __global__ __launch_bounds__(256) void grad_kernel(Logits S, int N, int c0, int 
                 const E q = to_elem(g[i][e], E());
                 g[i][e] -= from_elem(q);
                 tile[i * 16 + y][4 * x + e] = q;
-                if (out.G && n < N && c + e < cols) ((E*)out.G)[((int64_t)term * N + n) * out.ldg + c + e] = q;
+                if (out.G && n < (out.terms > 1 ? out.ldx : N) && c + e < cols)
+                    ((E*)out.G)[((int64_t)term * out.ldx + n) * out.ldg + c + e] = q;
             }
         }
         if (!out.GT) continue;
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(256) void fix_kernel(LossTargets t, const float* __
     for (int term = 0; term < out.terms; ++term) {
         const E q = to_elem(g, E());
         g -= from_elem(q);
-        if (out.G) ((E*)out.G)[((int64_t)term * N + n) * out.ldg + c] = q;
+        if (out.G) ((E*)out.G)[((int64_t)term * out.ldx + n) * out.ldg + c] = q;
         if (out.GT) ((E*)out.GT)[c * out.ldgt + term * out.ldx + n] = q;
     }
 }

@@ -69,8 +69,8 @@ hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, floa
 hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
                             float* r, float* scale, hipStream_t stream);
 // A piece of G, N rows and `cols` columns, and its transpose (either NULL: not wanted).
-// terms 2: bfloat16 entries as a sum of two, the second N rows on in G and ldx columns
-// on in GT (whose columns [N, ldx) are then zeros).
+// terms 2: bfloat16 entries as a sum of two, the second ldx rows on in G and ldx columns
+// on in GT; rows and columns [N, ldx) of either are then zeros.
 struct GradOut {
     void* G = nullptr;
     int64_t ldg = 0;

@@ -53,19 +53,22 @@ constexpr int64_t kRanges = 16, kRangeFloats = (int64_t)1 << 24;
 
 int most_ranges(int64_t R, int64_t ld) { return (int)std::max<int64_t>(1, std::min(kRanges, kRangeFloats / (R * ld))); }
 
-// How a gradient's product ends: from the tiles' epilogue (its `tile`), from the small
-// tiles' (their configuration), or as float32 sums that a pass of their own rounds.
-struct End {
-    enum { SUMS, EPILOGUE, SMALL } how = SUMS;
-    int tile = -1;
+// How a gradient's product runs: on the tiles that take W, or G, as it lies, ending in
+// the tiles' epilogue or in float32 sums of depth ranges; on the small tiles, ending
+// there too; or as float32 sums of transposed operands that a pass of their own rounds.
+struct Way {
+    enum { SUMS, SMALL, EPILOGUE, RANGES } how = SUMS;
+    int tile = -1;                // or the small tiles' configuration
+    int ranges = 1;
+    bool tiled() const { return how == EPILOGUE || how == RANGES; }
 };
-End end_of(const F32Plan& p) {
-    End e;
-    if (p.ranges == 1 && (p.kind == F32Plan::TILED || p.kind == F32Plan::MID)) {
-        e.how = p.kind == F32Plan::TILED ? End::EPILOGUE : End::SMALL;
-        e.tile = p.tile;
-    }
-    return e;
+Way way_of(const F32Plan& p) {
+    Way w;
+    if (p.kind == F32Plan::TILED) w.how = p.ranges == 1 ? Way::EPILOGUE : Way::RANGES;
+    else if (p.kind == F32Plan::MID && p.ranges == 1) w.how = Way::SMALL;
+    w.tile = p.tile;
+    w.ranges = p.ranges;
+    return w;
 }
 
 struct Layout {
@@ -75,8 +78,9 @@ struct Layout {
     int slab;                    // columns of their slabs
     int64_t P;                   // columns of a piece
     int terms;
-    End x, w;                    // of dX's and dW's products
+    Way x, w;                    // dX's and dW's products
     int ranges_s, ranges_x;      // of the logits' (tile < 0) and dX's (sums) products, at most
+    int64_t rows;                // of G, and of dX's sums: a second term's from ldn on
     int64_t ldn, ldp, ldk, ldfirst;
 };
 
@@ -133,26 +137,35 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     if (T > 0) b.mass = take((size_t)N * 4);
     b.r = take((size_t)N * 4);
     b.scale = take(4);
-    b.XT = take((size_t)K * b.ldn * b.terms * es);
-    b.G = take((size_t)N * b.terms * b.ldp * es);
-    b.GT = take((size_t)b.P * b.ldn * b.terms * es);
-    b.WT = take((size_t)K * b.ldp * es);
-    const int64_t rows = N * b.terms;
-    b.ranges_x = pieces <= 4 ? most_ranges(rows, b.ldk) : 1;
+    const int64_t ldgt = b.ldn * b.terms, depth = b.terms == 1 ? N : ldgt;
+    b.rows = depth;
+    b.ranges_x = pieces <= 4 ? most_ranges(b.rows, b.ldk) : 1;
     if (bf16) {
-        b.w = end_of(f32_plan(b.P, K, b.ldn * b.terms, b.ldn * b.terms, b.ldn * b.terms, 1));
-        if (b.terms == 1) b.x = end_of(f32_plan(N, K, b.P, b.ldp, b.ldp, b.ranges_x));
-        // the small tiles do not add to what is there
-        if (b.x.how == End::SMALL && pieces > 1) b.x = End{};
+        // (either operand order of dW's product has this price)
+        const F32Plan w = f32_plan(K, b.P, depth, ldgt, ldgt, 1), small = f32_plan(b.P, K, depth, ldgt, ldgt, 1);
+        b.w = w.kind == F32Plan::TILED ? way_of(w) : (small.kind == F32Plan::MID ? way_of(small) : Way{});
+        b.x = way_of(f32_plan(b.rows, K, b.P, b.ldp, b.ldp, b.ranges_x));
+        // two terms are added by the pass that rounds
+        if (b.terms > 1 && b.x.how == Way::EPILOGUE) b.x.how = Way::RANGES;
+        // the small tiles do not add to what is there, and the ranges of many pieces
+        // find no room
+        if ((b.x.how == Way::SMALL && (pieces > 1 || b.terms > 1)) || (b.x.how == Way::RANGES && pieces > 4)) b.x = Way{};
     }
-    // sums of dX: of more than one piece to be added to, or ranges, or two pieces'; a
-    // call whose leading dimensions take it to narrow pieces has two
+    // Narrow pieces, which take transposed operands and float32 sums, may be needed
+    // where the tiles are planned.
+    const bool tiles = b.tile >= 0 || b.x.tiled();
+    const int64_t narrow = ld8(std::min(V, kNarrow));
+    b.XT = take((size_t)K * ldgt * es);
+    b.G = take((size_t)b.rows * b.ldp * es);
+    b.GT = take((size_t)(b.w.tiled() ? narrow : b.P) * ldgt * es);
+    b.WT = take((size_t)K * (b.x.tiled() ? narrow : b.ldp) * es);
+    // sums of dX: of more than one piece to be added to, or ranges, or two pieces'
     int64_t sums = std::min<int64_t>(pieces, 2);
-    if (b.x.how != End::SUMS) sums = pieces > 1 ? 1 : 0;
+    if (b.x.how == Way::EPILOGUE || b.x.how == Way::SMALL) sums = pieces > 1 ? 1 : 0;
     else if (pieces <= 4) sums = b.ranges_x * pieces;
-    if (b.tile >= 0) sums = std::max<int64_t>(sums, 2);
-    b.acc = take((size_t)rows * b.ldk * 4 * sums);
-    b.out = take((size_t)(b.w.how != End::SUMS ? std::min(V, kNarrow) : b.P) * b.ldk * 4);
+    if (tiles) sums = std::max<int64_t>(sums, 2);
+    b.acc = take((size_t)b.rows * b.ldk * 4 * sums);
+    b.out = take((size_t)(b.w.how != Way::SUMS ? narrow : b.P) * b.ldk * 4);
     b.total = o;
     return b;
 }
@@ -306,15 +319,15 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     float* out = (float*)(ws + b.out);
     void *XT = ws + b.XT, *G = ws + b.G, *GT = ws + b.GT, *WT = ws + b.WT;
     const float inv_t = 1.f / temperature;
-    const bool fused = b.tile >= 0 && N * ldx < kLim && b.P * ldw < kLim;
-    // leading dimensions past the epilogues' offsets: narrow pieces and float32 sums
-    const bool narrow = b.tile >= 0 && !fused;
+    // leading dimensions past the tiles' offsets: narrow pieces and float32 sums
+    const bool narrow = (b.tile >= 0 && N * ldx >= kLim) || ((b.tile >= 0 || b.x.tiled()) && b.P * ldw >= kLim);
+    const bool fused = b.tile >= 0 && !narrow;
     const int64_t P = narrow ? std::min(V, kNarrow) : b.P;
     const int64_t pieces = (V + P - 1) / P;
-    const End ex = narrow ? End{} : b.x, ew = narrow ? End{} : b.w;
-    const int64_t rows = N * b.terms, slab = rows * b.ldk;      // of dX's sums
+    const Way wx = narrow ? Way{} : b.x, ww = narrow ? Way{} : b.w;
+    const int64_t slab = b.rows * b.ldk;                        // of dX's sums
     const bool many = pieces <= 4 && !narrow;                   // their ranges stay apart
-    const int64_t ldgt = b.ldn * b.terms;
+    const int64_t ldgt = b.ldn * b.terms, ldwt = ld8(P);
     // up to as many entries as a tile of G has columns: with the tile (its 64 tokens'
     // entries are looked through for each), else by a pass over the entries
     const bool few = !t.labels && !fused && t.T <= 64;
@@ -330,9 +343,9 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         const char* Wp = (const char*)W + (size_t)c0 * ldw * es;
         const bool last = c0 + cols == V;
         espace::GradOut go;
-        go.G = dX || fused ? G : nullptr;
+        go.G = dX || fused || ww.tiled() ? G : nullptr;
         go.ldg = b.ldp;
-        go.GT = dW ? GT : nullptr;
+        go.GT = dW && !ww.tiled() ? GT : nullptr;
         go.ldgt = ldgt;
         go.ldx = b.ldn;
         go.terms = b.terms;
@@ -344,7 +357,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             e.labels = t.labels;
             e.lse = lse;
             e.r = r;
-            e.GT = dW ? (uint16_t*)GT : nullptr;
+            e.GT = (uint16_t*)go.GT;
             e.ldgt = ldgt;
             ESPACE_TRY(run_tn_loss(X, ldx, Wp, ldw, G, b.ldp, N, cols, K, b.tile, espace::LOSS_GRAD, e, stream));
         } else {
@@ -357,21 +370,27 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
                                                                        (int)cols, go, stream));
         if (dX) {
-            ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, b.ldp, f32, stream));
-            if (ex.how == End::EPILOGUE) {
+            if (!wx.tiled())
+                ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, ldwt, f32, stream));
+            if (wx.how == Way::EPILOGUE) {
                 espace::LossEpi e;
                 e.acc = acc;
                 e.ldacc = b.ldk;
                 e.scale = scale;
                 e.add = c0 > 0;
                 e.last = last;
-                ESPACE_TRY(run_tn_loss(G, b.ldp, WT, b.ldp, dX, lddx, N, K, cols, ex.tile, espace::LOSS_GRAD_OUT, e,
+                ESPACE_TRY(run_tn_loss(G, b.ldp, Wp, ldw, dX, lddx, N, K, cols, wx.tile, espace::LOSS_GRAD_OUT, e,
                                        stream));
-            } else if (ex.how == End::SMALL) {
-                ESPACE_TRY(run_tn_scaled_mid(G, b.ldp, WT, b.ldp, dX, lddx, N, K, cols, ex.tile, scale, stream));
+            } else if (wx.how == Way::RANGES) {
+                int made = 1;
+                ESPACE_TRY(run_tiled_ranges(G, b.ldp, Wp, ldw, acc + sums * slab, b.rows, K, cols, wx.tile, wx.ranges,
+                                            &made, stream));
+                sums += made;
+            } else if (wx.how == Way::SMALL) {
+                ESPACE_TRY(run_tn_scaled_mid(G, b.ldp, WT, ldwt, dX, lddx, N, K, cols, wx.tile, scale, stream));
             } else {
                 int made = 1;
-                ESPACE_TRY(run_tn_f32(G, b.ldp, WT, b.ldp, acc + sums * slab, b.ldk, rows, K, cols, dt, stream,
+                ESPACE_TRY(run_tn_f32(G, b.ldp, WT, ldwt, acc + sums * slab, b.ldk, b.rows, K, cols, dt, stream,
                                       many ? b.ranges_x : 1, &made));
                 if (many || !sums) sums += made;
                 else ESPACE_LAUNCH("sum", espace::launch_add_f32(acc, acc + slab, slab, stream));
@@ -379,25 +398,25 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         }
         if (dW) {
             void* o = (char*)dW + (size_t)c0 * lddw * es;
-            const int64_t depth = b.terms > 1 ? b.ldn + N : N;
-            if (ew.how == End::EPILOGUE) {
+            const int64_t depth = b.rows;
+            if (ww.how == Way::EPILOGUE) {
                 espace::LossEpi e;
                 e.scale = scale;
                 e.last = 1;
-                ESPACE_TRY(run_tn_loss(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ew.tile, espace::LOSS_GRAD_OUT, e,
+                ESPACE_TRY(run_tn_loss(XT, ldgt, G, b.ldp, o, lddw, K, cols, depth, ww.tile, espace::LOSS_GRAD_OUT_T, e,
                                        stream));
-            } else if (ew.how == End::SMALL) {
-                ESPACE_TRY(run_tn_scaled_mid(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ew.tile, scale, stream));
+            } else if (ww.how == Way::SMALL) {
+                ESPACE_TRY(run_tn_scaled_mid(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ww.tile, scale, stream));
             } else {
                 ESPACE_TRY(run_tn_f32(GT, ldgt, XT, ldgt, out, b.ldk, cols, K, depth, dt, stream));
                 ESPACE_LAUNCH("gradient", espace::launch_sum_out(out, b.ldk, 1, 0, scale, o, lddw, cols, K, f32, stream));
             }
         }
     }
-    if (dX && ex.how == End::SUMS)
+    if (dX && (wx.how == Way::SUMS || wx.how == Way::RANGES))
         // a second term's rows are a slab of their own
-        ESPACE_LAUNCH("gradient", espace::launch_sum_out(acc, b.ldk, sums * b.terms, N * b.ldk, scale, dX, lddx, N, K,
-                                                         f32, stream));
+        ESPACE_LAUNCH("gradient", espace::launch_sum_out(acc, b.ldk, sums * b.terms, slab / b.terms, scale, dX, lddx, N,
+                                                         K, f32, stream));
     return ESPACE_OK;
 }
 

@@ -18,6 +18,7 @@ constexpr int V3_ROWB = 64;                       // bytes per half-stage row
 // Tile 256 x BN (BN = 256 or 192): each wave owns 128 x BN/2 as 8 x NBJ blocks.
 template <int BN>
 struct V3Cfg {
+    static constexpr int COLS = BN;
     static constexpr int NBJ = BN / 32;                   // 16-column blocks per wave tile
     static constexpr int ROWS = V3_BM + BN;               // A|B rows of a half-stage
     static constexpr int HS = ROWS * V3_ROWB;             // half-stage bytes (32 or 28 KB)
@@ -35,6 +36,18 @@ struct V3Cfg {
 };
 
 __device__ __forceinline__ int v3_swz(int r) { return (r >> 1) & 3; }
+
+// B in rows along its columns ("BT": element (k, c) at k ldb + c).  Its part of a
+// half-stage is then 32 depth rows of 2 BN bytes, and a fragment comes from two
+// transposing reads: ds_read_b64_tr_b16 gives lane i of 16 the i-th column of the 4 x 16
+// block whose rows i / 4 the lanes address 8 bytes each (measured lane by lane).  32-byte
+// chunk c of depth row r sits at c ^ v3_turn(r): the 16 rows that a read touches, 0 - 3, 8
+// - 11, 16 - 19 and 24 - 27 or those 4 on, fall two on each of the banks' eight groups
+// (of 192 columns, rows of 384 bytes already alternate between two halves).
+template <class C>
+__device__ __forceinline__ int v3_turn(int r) {
+    return C::COLS == 256 ? (r & 3) | ((r >> 1) & 4) : ((r >> 1) & 1) | ((r >> 2) & 2);
+}
 
 // s_waitcnt with one counter and the others left free (gfx9 encoding)
 __device__ __forceinline__ void v3_wait_lgkm0() { __builtin_amdgcn_s_waitcnt(0xC07F); }
@@ -97,18 +110,39 @@ __device__ __forceinline__ void v3_read_dyn(int x, bf16x8_t* fa, bf16x8_t* fb, u
 #undef V3_R
 }
 
+// The same with BT, x in the order fa0, fb0 .. fb(NBJ-1), fa1 ..: `ab` the lane's row
+// of B's part, turn[j] the byte of block j in it.
+template <class C>
+__device__ __forceinline__ void v3_read_bt(int x, bf16x8_t* fa, bf16x8_t* fb, unsigned aa, unsigned ab,
+                                           const int* turn) {
+#pragma unroll
+    for (int j = 0; j < C::NBJ; ++j)
+        if (x == 1 + j) {
+            // (the builtin would wait for the loads into LDS that are in flight)
+            u32x2_t lo, hi;
+            asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(lo) : "v"(ab + turn[j]));
+            asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(ab + turn[j]), "i"(4 * C::COLS * 2));
+            fb[j] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3));
+        }
+#define V3_A(n) if (x == (n == 0 ? 0 : C::NBJ + n)) V3_READ(fa[n], aa, n * 1024);
+    V3_A(0) V3_A(1) V3_A(2) V3_A(3) V3_A(4) V3_A(5) V3_A(6) V3_A(7)
+#undef V3_A
+}
+
 // Wave-load j of half h of depth step kt into half-stage u (full depth): it
 // covers rows 16q .. 16q+15 of the A|B tile, q = wave + 4j; j < 4 are A rows.
 // APAIR: A in the row-pair layout, where the 32-deep block of half h of step
 // kt lies (2 kt + h) * 128 bytes into a row pair (twice the plain offset).
-template <class C, bool APAIR = false>
+// BT: B in rows of ldb2 bytes along its columns, half-stage rows of 32 depths.
+template <class C, bool APAIR = false, bool BT = false>
 __device__ __forceinline__ void v3_load(unsigned char* smem, const uint16_t* A, const uint16_t* B,
                                         unsigned a_bytes, unsigned b_bytes, const int* voff,
-                                        int wave, int kt, int h, int u, int j) {
+                                        int wave, int kt, int h, int u, int j, unsigned ldb2 = 0) {
     const int q = wave + 4 * j;
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(j < 4 ? A : B), (short)0,
                                                         (int)(j < 4 ? a_bytes : b_bytes), 0x00020000);
-    const int soff = (kt * V3_BK + 32 * h) * ((APAIR && j < 4) ? 4 : 2);
+    const int soff = (BT && j >= 4) ? (int)((unsigned)(kt * V3_BK + 32 * h) * ldb2)
+                                    : (kt * V3_BK + 32 * h) * ((APAIR && j < 4) ? 4 : 2);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         rsrc, (__attribute__((address_space(3))) void*)(smem + u * C::HS + q * 1024), 16,
         voff[j], soff, 0, 0);
@@ -118,19 +152,32 @@ __device__ __forceinline__ void v3_load(unsigned char* smem, const uint16_t* A, 
 // buffer_load ... lds (8 per wave, returns 8), the depth tail through
 // registers with the elements at or beyond D zeroed (returns 0: nothing of
 // it stays in flight).
-template <class C, bool APAIR = false>
+// BT: rows of B past the depth are read from past the buffer (zeros), before A's part:
+// A's loads, which the registers wait for, are the newer ones.
+template <class C, bool APAIR = false, bool BT = false>
 __device__ __forceinline__ int v3_load_half(unsigned char* smem, const uint16_t* A, const uint16_t* B,
                                             unsigned a_bytes, unsigned b_bytes, const int* voff,
-                                            int wave, int lane, int kt, int h, int u, int D) {
+                                            int wave, int lane, int kt, int h, int u, int D, unsigned ldb2 = 0) {
     const int k0 = kt * V3_BK + 32 * h;
     if (k0 + 32 <= D) {
 #pragma unroll
         for (int j = 0; j < C::LPH; ++j)
-            v3_load<C, APAIR>(smem, A, B, a_bytes, b_bytes, voff, wave, kt, h, u, j);
+            v3_load<C, APAIR, BT>(smem, A, B, a_bytes, b_bytes, voff, wave, kt, h, u, j, ldb2);
         return C::LPH;
     }
+    if constexpr (BT) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)B, (short)0, (int)b_bytes, 0x00020000);
 #pragma unroll
-    for (int j = 0; j < C::LPH; ++j) {
+        for (int j = 4; j < C::LPH; ++j) {
+            const int q = wave + 4 * j;
+            const int row = ((q - 16) * 64 + lane) / (C::COLS / 8);
+            const unsigned off = k0 + row < D ? (unsigned)voff[j] + (unsigned)k0 * ldb2 : 0xFFFFFFF0u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc, (__attribute__((address_space(3))) void*)(smem + u * C::HS + q * 1024), 16, (int)off, 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < (BT ? 4 : C::LPH); ++j) {
         const int q = wave + 4 * j;
         const int rr = q * 16 + (lane >> 2) - (j < 4 ? 0 : V3_BM);
         const int lc = (lane & 3) ^ v3_swz(rr);
@@ -149,30 +196,38 @@ __device__ __forceinline__ int v3_load_half(unsigned char* smem, const uint16_t*
 // y of half h of step kt into half-stage u when LOADS and do_load (uniform);
 // FIRST: the accumulators start from zero (the inline constant 0 as the
 // addend).
-template <class C, bool FIRST, bool READS, bool LOADS, bool APAIR = false>
+// SWAP: the MFMA's operands change places (a lane then holds a column of B and 4 rows of
+// A of each block).
+template <class C, bool FIRST, bool READS, bool LOADS, bool APAIR = false, bool BT = false, bool SWAP = false>
 __device__ __forceinline__ void v3_substep(f32x4_t (&acc)[V3_NB][C::NBJ], const bf16x8_t* fa,
                                            const bf16x8_t* fb, bf16x8_t* ra, bf16x8_t* rb,
                                            unsigned aa, unsigned ab, unsigned char* smem,
                                            const uint16_t* A, const uint16_t* B, unsigned a_bytes,
                                            unsigned b_bytes, const int* voff, int wave, int kt,
-                                           int h, int u, bool do_load = true) {
+                                           int h, int u, bool do_load = true, unsigned ldb2 = 0,
+                                           const int* turn = nullptr) {
 #pragma unroll
     for (int i = 0; i < V3_NB; ++i)
 #pragma unroll
         for (int j = 0; j < C::NBJ; ++j) {
+            const bf16x8_t& p = SWAP ? fa[i] : fb[j];
+            const bf16x8_t& q = SWAP ? fb[j] : fa[i];
             if constexpr (FIRST)
                 asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0"
-                             : "=a"(acc[i][j]) : "v"(fb[j]), "v"(fa[i]));
+                             : "=a"(acc[i][j]) : "v"(p), "v"(q));
             else
-                V3_MFMA(acc[i][j], fb[j], fa[i]);
+                V3_MFMA(acc[i][j], p, q);
             const int x = i * C::NBJ + j;
-            if constexpr (READS)
+            if constexpr (READS && BT) {
+                if (x < 2 * (V3_NB + C::NBJ) && (x & 1) == 0) v3_read_bt<C>(x >> 1, ra, rb, aa, ab, turn);
+                __builtin_amdgcn_sched_barrier(0);
+            } else if constexpr (READS)
                 if (x < 2 * C::NRD && (x & 1) == 0) v3_read_dyn<C::NBJ>(x >> 1, ra, rb, aa, ab);
             if constexpr (LOADS) {
 #pragma unroll
                 for (int y = 0; y < C::LPH; ++y)
                     if (x == C::load_slot(y) && do_load)
-                        v3_load<C, APAIR>(smem, A, B, a_bytes, b_bytes, voff, wave, kt, h, u, y);
+                        v3_load<C, APAIR, BT>(smem, A, B, a_bytes, b_bytes, voff, wave, kt, h, u, y, ldb2);
             }
         }
 }
@@ -189,13 +244,21 @@ enum { V3_BF16 = 0, V3_F32 = 1, V3_PAIR = 2,
 // APAIR: A in the row-pair layout (lda its pair pitch); the four lanes of a
 // row then read one half of a 128-byte block whose other half the next
 // four lanes read for the row's partner, so a wave-load is 8 whole lines.
-template <class C, int SH = 1, bool APAIR = false>
+// BT: row and chunk of the depth rows of B (see v3_turn); those past the matrix's columns
+// read what follows, or zeros past its end.
+template <class C, int SH = 1, bool APAIR = false, bool BT = false>
 __device__ __forceinline__ void v3_offsets(int* voff, int row0, int col0, int R, int Cc, int64_t lda,
                                            int64_t ldb, int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < C::LPH; ++j) {
         const int q = wave + 4 * j;
         const bool isA = j < 4;
+        if (BT && !isA) {
+            const int at = (q - 16) * 64 + lane, row = at / (C::COLS / 8);
+            const int c = (at - row * (C::COLS / 8)) ^ (v3_turn<C>(row) << 1);
+            voff[j] = (int)(((unsigned)row * (unsigned)ldb + (unsigned)(col0 + c * 8)) * 2u);
+            continue;
+        }
         const int rr = q * 16 + (lane >> 2) - (isA ? 0 : V3_BM);
         const int lc = (lane & 3) ^ ((rr >> SH) & 3);
         int gr = (isA ? row0 : col0) + rr;
