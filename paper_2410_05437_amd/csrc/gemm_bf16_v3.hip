@@ -52,99 +52,102 @@ __device__ __forceinline__ float v3_over_row(float x, F f) {
     return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// The rows of a wave's 128 x BN/2 sub-tile are spread as elsewhere: block (i, j), row
-// 16 i + lane % 16, columns 16 j + 4 (lane / 16) + {0..3}.  row0, col0: the sub-tile's
-// first row and column; slab: its index among the slabs of BN/2 columns.
-// SWAP (MODE_GRAD_OUT, last, nothing to add): C is [Cc][R]; a lane holds column 16 j +
-// lane % 16 of block (i, j) and rows 16 i + 4 (lane / 16) + {0..3}.
+// Epilogues of a wave's 128 x BN/2 sub-tile at (row0, col0).
+// STATS and GRAD, swapped: rows are vocabulary entries, columns tokens; a lane holds, of
+// token block j, the token 16 j + lane % 16, and of vocabulary block i the entries 16 i
+// + 4 (lane / 16) + {0..3}.  slab: the sub-tile's among those of 128 entries.
+// GRAD_OUT: block (i, j), row 16 i + lane % 16, columns 16 j + 4 (lane / 16) + {0..3};
+// swapped (last, nothing to add): C is [Cc][R], a lane holds column 16 j + lane % 16 and
+// rows 16 i + 4 (lane / 16) + {0..3}.
 template <int MODE, int BN, bool SWAP, class EPI>
 __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3Cfg<BN>::NBJ], const EPI& epi,
                                                  void* Cout, int64_t ldc, int row0, int col0, int slab, int R, int Cc,
                                                  int lane, float* spare) {
     constexpr int NBJ = V3Cfg<BN>::NBJ;
+    static_assert(MODE == V3_GRAD_OUT || SWAP, "tokens are columns");
     const int lr = lane & 15, lh = lane >> 4;
-    const int c0 = col0 + 4 * lh;                 // of block j: + 16 j
     if constexpr (MODE == V3_STATS) {
+        const int v0 = row0 + 4 * lh;             // of block i: + 16 i
         const int entries = epi.T;
-        int lab[V3_NB];                           // the label's column in the sub-tile
-        int q0[V3_NB], q1[V3_NB];                 // the row's entries in the slab
+        int lab[NBJ];                             // the label's place in the slab
+        int q0[NBJ], q1[NBJ];                     // the token's entries in the slab
 #pragma unroll
-        for (int i = 0; i < V3_NB; ++i) {
-            const int r = min(row0 + 16 * i + lr, R - 1);
-            lab[i] = -1;
-            q0[i] = q1[i] = 0;
+        for (int j = 0; j < NBJ; ++j) {
+            const int n = min(col0 + 16 * j + lr, Cc - 1);
+            lab[j] = -1;
+            q0[j] = q1[j] = 0;
             if (epi.labels) {
-                const int64_t c = epi.labels[r] - epi.col0 - col0;
-                lab[i] = c >= 0 && c < BN / 2 && col0 + c < Cc ? (int)c : -1;
+                const int64_t c = epi.labels[n] - epi.col0 - row0;
+                lab[j] = c >= 0 && c < V3_WT && row0 + c < R ? (int)c : -1;
             } else if (entries) {
-                const int at = epi.col0 / (BN / 2) + slab;
-                q0[i] = epi.first[(int64_t)r * epi.ldfirst + at];
-                q1[i] = epi.first[(int64_t)r * epi.ldfirst + at + 1];
+                const int at = epi.col0 / V3_WT + slab;
+                q0[j] = epi.first[(int64_t)n * epi.ldfirst + at];
+                q1[j] = epi.first[(int64_t)n * epi.ldfirst + at + 1];
             }
         }
-        // each of a row's four lanes looks at one entry at a time
-        int col[V3_NB];
+        // each of a token's four lanes looks at one entry at a time
+        int col[NBJ];
 #pragma unroll
-        for (int i = 0; i < V3_NB; ++i) {
-            const int r = row0 + 16 * i + lr;
-            q0[i] += lh;
-            if (r >= R) q1[i] = 0;
-            col[i] = q0[i] < q1[i] ? epi.col[(int64_t)r * entries + q0[i]] : 0;
+        for (int j = 0; j < NBJ; ++j) {
+            const int n = col0 + 16 * j + lr;
+            q0[j] += lh;
+            if (n >= Cc) q1[j] = 0;
+            col[j] = q0[j] < q1[j] ? epi.col[(int64_t)n * entries + q0[j]] : 0;
         }
-        const bool whole = col0 + BN / 2 <= Cc;   // of the vocabulary
+        const bool whole = row0 + V3_WT <= R;     // of the vocabulary
         const float k = epi.inv_t * 1.44269504088896340736f;
 #pragma unroll
-        for (int i = 0; i < V3_NB; ++i) {
-            const int r = row0 + 16 * i + lr;
-            f32x4_t v[NBJ];
+        for (int j = 0; j < NBJ; ++j) {
+            const int n = col0 + 16 * j + lr;
+            f32x4_t v[V3_NB];
             float m = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < NBJ; ++j) {
-                v[j] = v3_acc_read(acc[i][j]);
+            for (int i = 0; i < V3_NB; ++i) {
+                v[i] = v3_acc_read(acc[i][j]);
                 if (!whole)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[j][e] = c0 + 16 * j + e < Cc ? v[j][e] : -INFINITY;
+                    for (int e = 0; e < 4; ++e) v[i][e] = v0 + 16 * i + e < R ? v[i][e] : -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m = fmaxf(m, v[j][e]);
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, v[i][e]);
             }
             m = v3_over_row(m, [](float a, float b) { return fmaxf(a, b); });
             // all -infinity: the sum stays 0, and NaN (which a maximum passes over) NaN
             const float base = m == -INFINITY ? 0.f : m;
             float l = 0.f;
 #pragma unroll
-            for (int j = 0; j < NBJ; ++j)
+            for (int i = 0; i < V3_NB; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f((v[j][e] - base) * k);
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f((v[i][e] - base) * k);
             l = v3_over_row(l, [](float a, float b) { return a + b; });
-            if (lh == 0 && r < R)
-                epi.part[(int64_t)slab * R + r] = make_float2(l == 0.f ? -INFINITY : base * epi.inv_t, l);
+            if (lh == 0 && n < Cc)
+                epi.part[(int64_t)slab * Cc + n] = make_float2(l == 0.f ? -INFINITY : base * epi.inv_t, l);
             if (epi.labels) {
-                if (__any(lab[i] >= 0) && lab[i] >= 0 && r < R && ((lab[i] >> 2) & 3) == lh) {
+                if (__any(lab[j] >= 0) && lab[j] >= 0 && n < Cc && ((lab[j] >> 2) & 3) == lh) {
                     float x = 0.f;
 #pragma unroll
-                    for (int j = 0; j < NBJ; ++j)
+                    for (int i = 0; i < V3_NB; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x = lab[i] == 16 * j + 4 * lh + e ? v[j][e] : x;
-                    epi.picked[(int64_t)r * epi.ldpk] = x * epi.inv_t;
+                        for (int e = 0; e < 4; ++e) x = lab[j] == 16 * i + 4 * lh + e ? v[i][e] : x;
+                    epi.picked[(int64_t)n * epi.ldpk] = x * epi.inv_t;
                 }
-            } else if (entries && __any(q0[i] < q1[i])) {
+            } else if (entries && __any(q0[j] < q1[j])) {
                 // the wave's own LDS, in the order of its instructions; 16-byte chunk c
-                // of row r at chunk c ^ r, so that the 16 rows of a write lie on
+                // of token t at chunk c ^ t, so that the 16 tokens of a write lie on
                 // distinct banks
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int j = 0; j < NBJ; ++j)
-                    *reinterpret_cast<f32x4_t*>(spare + lr * 128 + ((4 * j + lh) ^ lr) * 4) = v[j];
+                for (int i = 0; i < V3_NB; ++i)
+                    *reinterpret_cast<f32x4_t*>(spare + lr * 128 + ((4 * i + lh) ^ lr) * 4) = v[i];
                 __builtin_amdgcn_wave_barrier();
-                int q = q0[i], c = col[i];
-                while (__any(q < q1[i])) {
-                    if (q < q1[i]) {
-                        const int at = min(max(c - epi.col0 - col0, 0), BN / 2 - 1);
-                        epi.picked[(int64_t)r * epi.ldpk + epi.place[(int64_t)r * entries + q]] =
+                int q = q0[j], c = col[j];
+                while (__any(q < q1[j])) {
+                    if (q < q1[j]) {
+                        const int at = min(max(c - epi.col0 - row0, 0), V3_WT - 1);
+                        epi.picked[(int64_t)n * epi.ldpk + epi.place[(int64_t)n * entries + q]] =
                             spare[lr * 128 + ((at >> 2) ^ lr) * 4 + (at & 3)] * epi.inv_t;
                     }
                     q += 4;
-                    c = q < q1[i] ? epi.col[(int64_t)r * entries + q] : 0;
+                    c = q < q1[j] ? epi.col[(int64_t)n * entries + q] : 0;
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -152,7 +155,6 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
     } else {
         uint16_t* Cb = reinterpret_cast<uint16_t*>(Cout);
         // as in the bf16 epilogue: 8 consecutive columns a lane, for 2 blocks of 16
-        const int cl0 = col0 + 16 * (lh & 1) + 8 * (lh >> 1);   // + 32 m
         auto pack = [&](f32x4_t a, f32x4_t b) -> u32x4_t {
             const auto s0 = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false,
                                                              false);
@@ -161,88 +163,90 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
             return u32x4_t{s0[0], s1[0], s0[1], s1[1]};
         };
         if constexpr (MODE == V3_GRAD) {
-            const int Cc8 = (Cc + 7) & ~7;
+            const int R8 = (R + 7) & ~7;
             const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Cb, (short)0,
-                                                                (int)(unsigned)((uint64_t)R * ldc * 2u), 0x00020000);
-            float ls[V3_NB], rn[V3_NB];
-            int lab[V3_NB];
+                                                                (int)(unsigned)((uint64_t)Cc * ldc * 2u), 0x00020000);
+            const int v0 = row0 + 4 * lh;                            // of block i: + 16 i
+            const int v8 = row0 + 16 * (lh & 1) + 8 * (lh >> 1);     // of blocks 2 m, 2 m + 1: + 32 m
+            float ls[NBJ], rn[NBJ];
+            int lab[NBJ];
 #pragma unroll
-            for (int i = 0; i < V3_NB; ++i) {
-                const int r = min(row0 + 16 * i + lr, R - 1);
-                ls[i] = epi.lse[r];
-                rn[i] = epi.r[r];
-                lab[i] = -1;
+            for (int j = 0; j < NBJ; ++j) {
+                const int n = min(col0 + 16 * j + lr, Cc - 1);
+                ls[j] = epi.lse[n];
+                rn[j] = epi.r[n];
+                lab[j] = -1;
                 if (epi.labels) {
-                    const int64_t c = epi.labels[r] - epi.col0 - c0;
-                    lab[i] = c >= 0 && c < BN ? (int)c : -1;
+                    const int64_t c = epi.labels[n] - epi.col0 - v0;
+                    lab[j] = c >= 0 && c < V3_WT ? (int)c : -1;
                 }
             }
-            const bool whole = col0 + BN / 2 <= Cc;
+            const bool whole = row0 + V3_WT <= R;
             const float k = epi.inv_t * 1.44269504088896340736f;
             unsigned* turn = reinterpret_cast<unsigned*>(spare);
             const unsigned pick = (lr & 1) ? 0x03020706u : 0x05040100u;
 #pragma unroll
-            for (int h = 0; h < V3_NB / 2; ++h) {
+            for (int h = 0; h < NBJ / 2; ++h) {
 #pragma unroll
-                for (int ii = 0; ii < 2; ++ii) {
-                    const int i = 2 * h + ii, r = row0 + 16 * i + lr;
-                    const float shift = ls[i] * 1.44269504088896340736f;
-                    const unsigned live = rn[i] == 0.f ? 0u : 0xffffffffu;
-                    const bool labelled = __any(lab[i] >= 0 && lab[i] < BN / 2);
-                    unsigned w[NBJ][2];
+                for (int jj = 0; jj < 2; ++jj) {
+                    const int j = 2 * h + jj, n = col0 + 16 * j + lr;
+                    const float shift = ls[j] * 1.44269504088896340736f;
+                    const unsigned live = rn[j] == 0.f ? 0u : 0xffffffffu;
+                    const bool labelled = __any(lab[j] >= 0);
+                    unsigned w[V3_NB][2];
 #pragma unroll
-                    for (int j = 0; j < NBJ; ++j) {
+                    for (int i = 0; i < V3_NB; ++i) {
                         f32x4_t x = v3_acc_read(acc[i][j]);
                         // the exponent's rounding, 2^-24 of |s| + |lse|, is far below bfloat16's
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], k, -shift));
                         if (labelled)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[e] = lab[i] == 16 * j + e ? x[e] - 1.f : x[e];
+                            for (int e = 0; e < 4; ++e) x[e] = lab[j] == 16 * i + e ? x[e] - 1.f : x[e];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] *= rn[i];
+                        for (int e = 0; e < 4; ++e) x[e] *= rn[j];
                         if (!whole)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[e] = c0 + 16 * j + e < Cc ? x[e] : 0.f;
+                            for (int e = 0; e < 4; ++e) x[e] = v0 + 16 * i + e < R ? x[e] : 0.f;
                         // a token without a target: 0 whatever its logits are
-                        w[j][0] = pack_bf16x2(x[0], x[1]) & live;
-                        w[j][1] = pack_bf16x2(x[2], x[3]) & live;
+                        w[i][0] = pack_bf16x2(x[0], x[1]) & live;
+                        w[i][1] = pack_bf16x2(x[2], x[3]) & live;
                     }
 #pragma unroll
-                    for (int m = 0; m < NBJ / 2; ++m) {
+                    for (int m = 0; m < V3_NB / 2; ++m) {
                         const auto s0 = __builtin_amdgcn_permlane16_swap(w[2 * m][0], w[2 * m + 1][0], false, false);
                         const auto s1 = __builtin_amdgcn_permlane16_swap(w[2 * m][1], w[2 * m + 1][1], false, false);
-                        const int c = cl0 + 32 * m;
+                        const int c = v8 + 32 * m;
                         const unsigned off =
-                            (r < R && c < Cc8) ? ((unsigned)r * (unsigned)ldc + (unsigned)c) * 2u : 0xFFFFFFF0u;
+                            (n < Cc && c < R8) ? ((unsigned)n * (unsigned)ldc + (unsigned)c) * 2u : 0xFFFFFFF0u;
                         __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{s0[0], s1[0], s0[1], s1[1]}, rsrc, (int)off, 0,
                                                                0);
                     }
                     if (!epi.GT) continue;
-                    // two rows of a column in a word: the even lane of two neighbours
-                    // takes their first column, the odd one their second.  The words of
-                    // a column's 32 rows are 64 bytes of the wave's LDS, their 16-byte
-                    // chunk c at c ^ (column / 4): at most two lanes on a bank
+                    // two tokens of an entry in a word: the even lane of two neighbours
+                    // takes their first entry, the odd one their second.  The words of
+                    // an entry's 32 tokens are 64 bytes of the wave's LDS, their 16-byte
+                    // chunk c at c ^ (entry / 4): at most two lanes on a bank
 #pragma unroll
-                    for (int j = 0; j < NBJ; ++j)
+                    for (int i = 0; i < V3_NB; ++i)
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            const unsigned other = __builtin_amdgcn_mov_dpp(w[j][u], 0xB1, 0xF, 0xF, true);
-                            const int c = 16 * j + 4 * lh + 2 * u + (lr & 1);
-                            turn[c * 16 + (((2 * ii + (lr >> 3)) ^ lh) << 2) + ((lr >> 1) & 3)] =
-                                __builtin_amdgcn_perm(other, w[j][u], pick);
+                            const unsigned other = __builtin_amdgcn_mov_dpp(w[i][u], 0xB1, 0xF, 0xF, true);
+                            const int c = 16 * i + 4 * lh + 2 * u + (lr & 1);
+                            turn[c * 16 + (((2 * jj + (lr >> 3)) ^ lh) << 2) + ((lr >> 1) & 3)] =
+                                __builtin_amdgcn_perm(other, w[i][u], pick);
                         }
                 }
                 if (!epi.GT) continue;
                 __builtin_amdgcn_wave_barrier();  // the wave's own LDS, in order
 #pragma unroll
-                for (int q = 0; q < BN / 32; ++q) {
-                    const int c = 16 * q + (lane >> 2), n = row0 + 32 * h + 8 * (lane & 3);
+                for (int q = 0; q < V3_NB; ++q) {
+                    const int c = 16 * q + (lane >> 2), n = col0 + 32 * h + 8 * (lane & 3);
                     const u32x4_t v =
                         *reinterpret_cast<const u32x4_t*>(turn + c * 16 + (((lane & 3) ^ ((c >> 2) & 3)) << 2));
                     // rows of GT are padded to a multiple of 8
-                    if (n < R && col0 + c < Cc)
-                        *reinterpret_cast<u32x4_t*>(epi.GT + (int64_t)(col0 + c) * epi.ldgt + n) = v;
+                    if (n < Cc && row0 + c < R)
+                        *reinterpret_cast<u32x4_t*>(epi.GT + (int64_t)(row0 + c) * epi.ldgt + n) = v;
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -269,6 +273,8 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
             }
         } else {
             const float a = epi.last ? epi.scale[0] : 1.f;
+            const int c0 = col0 + 4 * lh;                            // of block j: + 16 j
+            const int cl0 = col0 + 16 * (lh & 1) + 8 * (lh >> 1);    // of blocks 2 m, 2 m + 1: + 32 m
 #pragma unroll
             for (int i = 0; i < V3_NB; ++i) {
                 const int r = row0 + 16 * i + lr;
@@ -380,9 +386,10 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
     const unsigned slot = (unsigned)((lh ^ v3_swz(lr)) * 16);
     const unsigned arow = sbase + (unsigned)((wrow0 + lr) * V3_ROWB) + slot;
     // depth-major B: the lane's depth row 8 lh + lr / 4, 8 bytes lr % 4 of each 16-column
-    // block, whose places in the row are turn[]
+    // block, whose places in the row are turn[] (v3_read_bt for 256 columns)
     const int trow = 8 * lh + (lr >> 2);
-    const unsigned brow = T ? sbase + (unsigned)(V3_BM * V3_ROWB + trow * BN * 2 + (lr & 3) * 8)
+    const unsigned brow = T ? sbase + (unsigned)(V3_BM * V3_ROWB + trow * BN * 2 + (lr & 3) * 8) +
+                                  (BN == 256 ? (unsigned)((wcol0 / 16) ^ v3_turn<C>(trow)) * 32u : 0u)
                             : sbase + (unsigned)((V3_BM + wcol0 + lr) * V3_ROWB) + slot;
     int turn[NBJ];
 #pragma unroll
@@ -541,7 +548,7 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
         // columns wcol0 + 16 j + 4 lh + {0..3}
         if constexpr (LOSS) {
             v3_loss_epilogue<MODE, BN, SWAP>(acc, epi, Cout, ldc, row0 + wrow0, col0 + wcol0,
-                                       (tile_c * BN + wcol0) / (BN / 2), R, Cc, lane, spare + (SPARE ? wave * 16 * 128 : 0));
+                                       (row0 + wrow0) / V3_WT, R, Cc, lane, spare + (SPARE ? wave * 16 * 128 : 0));
         } else {
         float* tpart = nullptr;
         unsigned long long* tstate = nullptr;
@@ -766,8 +773,8 @@ static hipError_t launch_loss(const GemmArgs& g, LossMode mode, const LossEpi& e
                        g.C, g.ldc, g.R, g.Cc, g.D, tiles_c, ntiles, ktiles, (int64_t)0, map, nullptr, nullptr, 0ull,  \
                        g.wait, 0, epi)
     switch (mode) {
-        case LOSS_STATS: LAUNCH(V3_STATS, V3_B_ROWS); break;
-        case LOSS_GRAD: LAUNCH(V3_GRAD, V3_B_ROWS); break;
+        case LOSS_STATS: LAUNCH(V3_STATS, V3_B_SWAPPED); break;
+        case LOSS_GRAD: LAUNCH(V3_GRAD, V3_B_SWAPPED); break;
         case LOSS_GRAD_OUT: LAUNCH(V3_GRAD_OUT, V3_B_DEPTH); break;
         case LOSS_GRAD_OUT_T: LAUNCH(V3_GRAD_OUT, V3_B_SWAPPED); break;
     }
@@ -777,9 +784,8 @@ static hipError_t launch_loss(const GemmArgs& g, LossMode mode, const LossEpi& e
 
 hipError_t launch_gemm_tn_bf16_loss(const GemmArgs& g, LossMode mode, const LossEpi& epi, hipStream_t stream) {
     const int64_t lim = (int64_t)1 << 31;
-    const bool depth = mode == LOSS_GRAD_OUT || mode == LOSS_GRAD_OUT_T;
-    if ((int64_t)g.R * g.lda >= lim || (int64_t)(depth ? g.D : g.Cc) * g.ldb >= lim || g.D < 1 ||
-        (mode == LOSS_GRAD && (int64_t)g.R * g.ldc >= lim) ||
+    if ((int64_t)g.R * g.lda >= lim || (int64_t)g.D * g.ldb >= lim || g.D < 1 ||
+        (mode == LOSS_GRAD && (int64_t)g.Cc * g.ldc >= lim) ||
         (mode == LOSS_GRAD_OUT_T && (epi.add || !epi.last)))
         return hipErrorInvalidValue;
     switch (g.tile) {

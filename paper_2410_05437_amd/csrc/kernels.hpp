@@ -96,25 +96,28 @@ hipError_t launch_gemm_tn_bf16_v2(const GemmArgs& g, hipStream_t stream);
 // 2^31 elements or more.
 constexpr int V4_MIN_STEPS = 48;
 hipError_t launch_gemm_tn_bf16_v4(const GemmArgs& g, hipStream_t stream);
-// What a product of a loss on a head's logits does with its sums s (float32, columns
-// col0 on of the vocabulary):
-//  stats     nothing is written but, of each 128 columns (96 with 192-column tiles),
-//            the largest s·inv_t and Σ exp(s·inv_t - it) of every row, at part[k·R + row]
-//            for the k-th such slab, and s·inv_t of the targets
-//  grad      C = r[row]·(exp(s·inv_t - lse[row]) - [column = labels[row]]) in bfloat16,
-//            0 where r is 0, zeros up to a multiple of 8 columns
-//  grad_out  a gradient, with B as [D][Cc]: acc (if add) + s is stored in acc, or times
-//            scale[0] in C in bfloat16 (if last)
+// What a product of a loss on a head's logits does with its sums s (float32).  B is
+// [D][Cc] in all of them.
+//  stats     A = a piece of W, B = X transposed: rows are vocabulary entries from col0
+//            on, columns tokens.  Nothing is written but, of each LOSS_SLAB entries, the
+//            largest s·inv_t and Σ exp(s·inv_t - it) of every token, at part[k·Cc +
+//            token] for the k-th such slab, and s·inv_t of the targets
+//  grad      the same operands; C [Cc][R] = r[token]·(exp(s·inv_t - lse[token]) - [entry
+//            = labels[token]]) in bfloat16, 0 where r is 0, zeros up to a multiple of 8
+//            entries
+//  grad_out  a gradient: acc (if add) + s is stored in acc, or times scale[0] in C in
+//            bfloat16 (if last)
 //  grad_out_t  the same, last and not added to anything, C written as [Cc][R]
+constexpr int LOSS_SLAB = 128;
 struct LossEpi {
     float inv_t = 1.f;
     int col0 = 0;
-    const int64_t* labels = nullptr;       // of the rows; NULL: entries, or none
+    const int64_t* labels = nullptr;       // of the tokens; NULL: entries, or none
     float2* part = nullptr;
-    float* picked = nullptr;               // of labels: [row]; of entries: [row][entry]
+    float* picked = nullptr;               // [token], or [token][place]
     int64_t ldpk = 1;
-    // T entries a row in the order of their columns (col) with their places (place)
-    // among the row's, and how many of them lie before each slab (first[row][slab])
+    // T entries a token in the order of their columns (col) with their places (place)
+    // among the token's, and how many of them lie before each slab (first[token][slab])
     const int* col = nullptr;
     const uint16_t* place = nullptr;
     const uint16_t* first = nullptr;
@@ -122,7 +125,7 @@ struct LossEpi {
     int T = 0;
     const float* lse = nullptr;
     const float* r = nullptr;
-    uint16_t* GT = nullptr;                // C's transpose, if wanted (rows padded to 8 elements)
+    uint16_t* GT = nullptr;                // C's transpose [R][Cc], if wanted (rows padded to 8)
     int64_t ldgt = 0;
     float* acc = nullptr;
     int64_t ldacc = 0;
@@ -130,9 +133,8 @@ struct LossEpi {
     int add = 0, last = 0;
 };
 enum LossMode { LOSS_STATS, LOSS_GRAD, LOSS_GRAD_OUT, LOSS_GRAD_OUT_T };
-// 256 x 256 and 256 x 192 plans (g.tile) with these epilogues; loss_slab: the columns
-// of a slab of the tile.  hipErrorInvalidValue for matrices of 2^31 elements or more.
-inline int loss_slab(int tile) { return tile == TILE_256x192 ? 96 : 128; }
+// 256 x 256 and 256 x 192 plans (g.tile) with these epilogues.  hipErrorInvalidValue for
+// matrices of 2^31 elements or more.
 hipError_t launch_gemm_tn_bf16_loss(const GemmArgs& g, LossMode mode, const LossEpi& epi, hipStream_t stream);
 // Four-wave 256 x 256 and 256 x 192 kernel with a hand-ordered main loop;
 // hipErrorInvalidValue for products it does not take (other tiles, fp32

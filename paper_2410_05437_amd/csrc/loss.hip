@@ -127,10 +127,10 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict_
                 there += __popcll(__ballot(c[u] >= 0));
             }
             __builtin_amdgcn_wave_barrier();      // the wave's own LDS, in order
-            const int slabs = (V + out.slab - 1) / out.slab;
+            const int slabs = (V + LOSS_SLAB - 1) / LOSS_SLAB;
             for (int s = lane; s <= slabs + 1; s += 64) {     // (a tile may end a slab later)
-                // entries before column s·slab
-                const int64_t edge = (int64_t)s * out.slab;
+                // entries before the slab
+                const int64_t edge = (int64_t)s * LOSS_SLAB;
                 int lo = 0, hi = there;
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;

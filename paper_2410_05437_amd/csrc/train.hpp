@@ -32,13 +32,12 @@ struct TeacherOut {
     // without a target
     float* mass = nullptr;
     // wanted for LossEpi: the entries in the order of their columns, their places, and
-    // how many lie before each slab of `slab` columns, up to the second past the last
-    // (rows ldfirst apart)
+    // how many lie before each LOSS_SLAB columns, up to the second past the last (rows
+    // ldfirst apart)
     int* sorted = nullptr;
     uint16_t* place = nullptr;
     uint16_t* first = nullptr;
     int64_t ldfirst = 0;
-    int slab = 1;
 };
 hipError_t launch_teacher(const int64_t* index, int64_t ldi, const float* logits, int64_t ldl, int N, int T, int V,
                           float inv_t, const TeacherOut& out, hipStream_t stream);

@@ -75,7 +75,6 @@ struct Layout {
     size_t S, part, picked, col, p, logp, sorted, place, first;    // forward (S, col, p: both)
     size_t mass, r, scale, XT, G, GT, WT, acc, out, total;         // backward
     int tile;                    // >= 0: the logits' epilogues on this tile
-    int slab;                    // columns of their slabs
     int64_t P;                   // columns of a piece
     int terms;
     Way x, w;                    // dX's and dW's products
@@ -98,7 +97,7 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     b.P = backward ? piece_cols(N, V, kGrads) : V;
     b.tile = -1;
     if (bf16 && b.terms == 1) {
-        const F32Plan p = f32_plan(N, b.P, K, ld8(K), ld8(K), 1);
+        const F32Plan p = f32_plan(b.P, N, K, ld8(K), ld8(K), 1);
         if (p.kind == F32Plan::TILED) b.tile = p.tile;
     }
     b.ranges_s = 1;
@@ -106,15 +105,16 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
         b.P = piece_cols(N, V, kLogits);
         b.ranges_s = most_ranges(N, espace::splitk_ld((int)b.P));
     }
-    b.slab = espace::loss_slab(b.tile);
     b.S = take((size_t)N * espace::splitk_ld((int)(b.tile < 0 ? b.P : std::min(V, kNarrow))) * 4 * b.ranges_s);
     if (T > 0) {
         b.col = take((size_t)N * T * 4);
         b.p = take((size_t)N * T * 4);
     }
+    b.ldn = ld8(N);
     if (!backward) {
+        if (b.tile >= 0) b.XT = take((size_t)K * b.ldn * es);
         const int64_t pieces = (V + b.P - 1) / b.P, stats = (b.P + espace::STAT_COLS - 1) / espace::STAT_COLS;
-        const int64_t slabs = (V + b.slab - 1) / b.slab;
+        const int64_t slabs = (V + espace::LOSS_SLAB - 1) / espace::LOSS_SLAB;
         b.part = take((size_t)N * (b.tile < 0 ? pieces * stats : std::max(slabs + 1, (V + kNarrow - 1) / kNarrow)) * 8);
         if (T > 0) {
             b.logp = take((size_t)N * T * 4);
@@ -131,7 +131,6 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
         return b;
     }
     const int64_t pieces = (V + b.P - 1) / b.P;
-    b.ldn = ld8(N);
     b.ldp = ld8(b.P);
     b.ldk = espace::splitk_ld((int)K);
     if (T > 0) b.mass = take((size_t)N * 4);
@@ -259,19 +258,21 @@ espace_status loss_forward(const void* X, int64_t ldx, const void* W, int64_t ld
     float2* part = (float2*)(ws + b.part);
     const float inv_t = 1.f / temperature;
     int parts = 0;
-    // the epilogue's launches: rows of W below 2^31 elements, in whole slabs of either width
-    const int64_t step = 768;
-    const bool fused = b.tile >= 0 && N * ldx < kLim && std::min(V, step) * ldw < kLim;
+    // the epilogue's launches: rows of W below 2^31 elements, in whole slabs
+    const int64_t step = 256;
+    const bool fused = b.tile >= 0 && K * b.ldn < kLim && std::min(V, step) * ldw < kLim;
     log_plan(b, false, fused, N, K, V, t.labels ? 0 : t.T, fused ? V : (b.tile >= 0 ? std::min(V, kNarrow) : b.P));
     if (fused) {
         const int64_t most = V * ldw < kLim ? V : (kLim - 1) / ldw / step * step;
+        void* XT = ws + b.XT;
+        ESPACE_LAUNCH("transpose", espace::launch_transpose(X, ldx, (int)N, (int)K, XT, b.ldn, false, stream));
         for (int64_t c0 = 0; c0 < V; c0 += most) {
             const int64_t cols = std::min(most, V - c0);
             espace::LossEpi e;
             e.inv_t = inv_t;
             e.col0 = (int)c0;
             e.labels = t.labels;
-            e.part = part + (size_t)(c0 / b.slab) * N;
+            e.part = part + (size_t)(c0 / espace::LOSS_SLAB) * N;
             e.picked = picked;
             e.ldpk = ldpk;
             if (!t.labels) {
@@ -281,10 +282,10 @@ espace_status loss_forward(const void* X, int64_t ldx, const void* W, int64_t ld
                 e.ldfirst = b.ldfirst;
                 e.T = t.T;
             }
-            ESPACE_TRY(run_tn_loss(X, ldx, (const uint16_t*)W + c0 * ldw, ldw, nullptr, 0, N, cols, K, b.tile,
+            ESPACE_TRY(run_tn_loss((const uint16_t*)W + c0 * ldw, ldw, XT, b.ldn, nullptr, 0, cols, N, K, b.tile,
                                    espace::LOSS_STATS, e, stream));
         }
-        parts = (int)((V + b.slab - 1) / b.slab);
+        parts = (int)((V + espace::LOSS_SLAB - 1) / espace::LOSS_SLAB);
     } else {
         const int64_t P = b.tile >= 0 ? std::min(V, kNarrow) : b.P;
         for (int64_t c0 = 0; c0 < V; c0 += P) {
@@ -320,7 +321,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     void *XT = ws + b.XT, *G = ws + b.G, *GT = ws + b.GT, *WT = ws + b.WT;
     const float inv_t = 1.f / temperature;
     // leading dimensions past the tiles' offsets: narrow pieces and float32 sums
-    const bool narrow = (b.tile >= 0 && N * ldx >= kLim) || ((b.tile >= 0 || b.x.tiled()) && b.P * ldw >= kLim);
+    const bool narrow = (b.tile >= 0 || b.x.tiled()) && (b.P * ldw >= kLim || K * b.ldn * b.terms >= kLim);
     const bool fused = b.tile >= 0 && !narrow;
     const int64_t P = narrow ? std::min(V, kNarrow) : b.P;
     const int64_t pieces = (V + P - 1) / P;
@@ -335,7 +336,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     log_plan(b, true, fused, N, K, V, t.labels ? 0 : t.T, P);
     ESPACE_LAUNCH("loss coefficients", espace::launch_loss_coef(dloss, t.labels, mass, temperature, (int)N, (int)V, r,
                                                                 scale, stream));
-    if (dW)
+    if (dW || fused)
         ESPACE_LAUNCH("transpose", espace::launch_transpose_live(X, ldx, r, (int)N, (int)K, XT, ldgt, b.ldn, b.terms,
                                                                  f32, stream));
     for (int64_t c0 = 0; c0 < V; c0 += P) {
@@ -359,7 +360,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             e.r = r;
             e.GT = (uint16_t*)go.GT;
             e.ldgt = ldgt;
-            ESPACE_TRY(run_tn_loss(X, ldx, Wp, ldw, G, b.ldp, N, cols, K, b.tile, espace::LOSS_GRAD, e, stream));
+            ESPACE_TRY(run_tn_loss(Wp, ldw, XT, ldgt, G, b.ldp, cols, N, K, b.tile, espace::LOSS_GRAD, e, stream));
         } else {
             espace::Logits s;
             ESPACE_TRY(logits_piece(X, ldx, W, ldw, S, N, K, c0, cols, dt, b.ranges_s, &s, stream));
@@ -458,7 +459,6 @@ espace_status forward(const void* X, int64_t ldx, const void* W, int64_t ldw, co
             to.place = (uint16_t*)(ws + b.place);
             to.first = (uint16_t*)(ws + b.first);
             to.ldfirst = b.ldfirst;
-            to.slab = b.slab;
         }
         ESPACE_LAUNCH("teacher", espace::launch_teacher(index, ldi, logits, ldl, (int)N, (int)T, (int)V,
                                                         1.f / temperature, to, stream));

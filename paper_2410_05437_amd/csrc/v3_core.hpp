@@ -120,8 +120,10 @@ __device__ __forceinline__ void v3_read_bt(int x, bf16x8_t* fa, bf16x8_t* fb, un
         if (x == 1 + j) {
             // (the builtin would wait for the loads into LDS that are in flight)
             u32x2_t lo, hi;
-            asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(lo) : "v"(ab + turn[j]));
-            asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(ab + turn[j]), "i"(4 * C::COLS * 2));
+            // 512-byte rows: `ab` holds block 0's place, and block j's differs in 32 j's bits
+            const unsigned at = C::COLS == 256 ? ab ^ (32u * j) : ab + turn[j];
+            asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(lo) : "v"(at));
+            asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(at), "i"(4 * C::COLS * 2));
             fb[j] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3));
         }
 #define V3_A(n) if (x == (n == 0 ? 0 : C::NBJ + n)) V3_READ(fa[n], aa, n * 1024);
