@@ -768,7 +768,7 @@ GemmArgs f32_args(const void* A, int64_t lda, const void* B, int64_t ldb, void* 
 
 }  // namespace
 
-F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges) {
+F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges, bool depth) {
     const int64_t lim = (int64_t)1 << 31;
     const int cus = device_cus();
     const double byte_cost = 315.0 / (2.0 * 64 * cus);
@@ -787,7 +787,7 @@ F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int
     for (const int bn : {256, 192})
         for (int s = 1; s <= ranges && (s == 1 || ktiles / s >= 8); ++s) {
             const int64_t rounds = ceil_div((int64_t)ceil_div(R, 256) * ceil_div(Cc, bn) * s, cus);
-            double c = rounds * (256.0 * bn * ceil_div(ktiles, s) / (bn == 256 ? 1.0 : 0.933) + 101e3);
+            double c = rounds * (256.0 * bn * ceil_div(ktiles, s) * (depth ? 0.88 : 1.0) / (bn == 256 ? 1.0 : 0.933) + 101e3);
             if (s > 1) c += 97e3 + 1.37 * s * (double)R * Cc * 4.0 * byte_cost;
             if (4.75 + kUnitUs * c >= best) continue;
             best = 4.75 + kUnitUs * c;

@@ -97,7 +97,7 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     b.P = backward ? piece_cols(N, V, kGrads) : V;
     b.tile = -1;
     if (bf16 && b.terms == 1) {
-        const F32Plan p = f32_plan(b.P, N, K, ld8(K), ld8(K), 1);
+        const F32Plan p = f32_plan(b.P, N, K, ld8(K), ld8(K), 1, true);
         if (p.kind == F32Plan::TILED) b.tile = p.tile;
     }
     b.ranges_s = 1;
@@ -141,9 +141,9 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     b.ranges_x = pieces <= 4 ? most_ranges(b.rows, b.ldk) : 1;
     if (bf16) {
         // (either operand order of dW's product has this price)
-        const F32Plan w = f32_plan(K, b.P, depth, ldgt, ldgt, 1), small = f32_plan(b.P, K, depth, ldgt, ldgt, 1);
+        const F32Plan w = f32_plan(K, b.P, depth, ldgt, ldgt, 1, true), small = f32_plan(b.P, K, depth, ldgt, ldgt, 1);
         b.w = w.kind == F32Plan::TILED ? way_of(w) : (small.kind == F32Plan::MID ? way_of(small) : Way{});
-        b.x = way_of(f32_plan(b.rows, K, b.P, b.ldp, b.ldp, b.ranges_x));
+        b.x = way_of(f32_plan(b.rows, K, b.P, b.ldp, b.ldp, b.ranges_x, true));
         // two terms are added by the pass that rounds
         if (b.terms > 1 && b.x.how == Way::EPILOGUE) b.x.how = Way::RANGES;
         // the small tiles do not add to what is there, and the ranges of many pieces

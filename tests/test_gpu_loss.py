@@ -377,3 +377,30 @@ def test_a_retraining_step(E):
         off = float((got.double() - want).norm() / want.norm())
         assert off <= 12 * step, (name, off)
     assert not dE[torch.bincount(tokens[tokens >= 0], minlength=V) == 0].any()
+
+
+@pytest.mark.parametrize("T", [0, 3])
+def test_leading_dimensions_past_the_tiles_offsets(E, T):
+    """A head whose rows lie so far apart that it spans 2^31 elements and more."""
+    N, K, V, t = 4300, 72, 9001, 2.0 if T else 1.0
+    X, W, g = _head(N, K, V, BF16, seed=10)
+    apart = (1 << 31) // V + 9 & ~7
+    far = torch.zeros((V * apart,), dtype=BF16, device="cuda").as_strided((V, K), (apart, 1))
+    far.copy_(W)
+    w = _weight(N, g)
+    if T:
+        index, logits = _teacher(N, V, T, g)
+        loss, lse, picked = E.espace_linear_distillation(X, far, index, logits, t)
+        dX, dW = E.espace_linear_distillation_backward(w, X, far, index, logits, lse, picked, t)
+        ref = R.Loss(X, W, index=index, logits=logits, t=t)
+        R.within(picked, ref.picked, ref.dpicked, "picked")
+    else:
+        labels = _labels(N, V, g)
+        loss, lse = E.espace_linear_cross_entropy(X, far, labels)
+        dX, dW = E.espace_linear_cross_entropy_backward(w, X, far, labels, lse)
+        ref = R.Loss(X, W, labels=labels)
+    R.within(lse[:, None], ref.lse, ref.dlse, "lse")
+    R.within(loss, ref.loss, ref.dloss, "loss")
+    rX, bX, rW, bW = ref.grads(w, False)
+    R.within(dX, rX, bX, "dX")
+    R.within(dW, rW, bW, "dW")
