@@ -61,8 +61,9 @@ struct F32Plan {
     int ranges = 1;
 };
 // depth: with B as [D][Cc] on the tiles, which are then faster (16384 deep, 4096 x 4096
-// 390 us where the others' price is 419).
-F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges, bool depth = false);
+// 390 us where the others' price is 419).  extra: us that the small tiles cost besides.
+F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges, bool depth = false,
+                 double extra = 0);
 // The float32 sums of plan.ranges depth ranges on the tiles of a plan of kind TILED, with
 // B as [D][Cc]; *made of them, R·splitk_ld(Cc) apart.
 espace_status run_tiled_ranges(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t R, int64_t Cc,

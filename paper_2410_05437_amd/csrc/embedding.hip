@@ -1,10 +1,9 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 //
 // Lookup: bound by the rows it copies.  A thread moves 16 bytes of a row.  Outputs
-// larger than the L2s together (32 MB) are written past them, here and for the
-// gradient's zero rows: 8192 rows of 6144 34.7 -> 24.2 us (8.3 TB/s of rows in and out,
-// many of them read again from a cache), the gradient of 4096 tokens on 32000 x 4096
-// 73.5 -> 60 us.
+// larger than the L2s together (32 MB) are written past them: 8192 rows of 6144 of a
+// text 34.7 -> 24.2 us (8.3 TB/s in and out, many rows read again from a cache), 16384
+// random rows 76.8 -> 68.3, 34 MB 12.2 -> 11.9.
 //
 // Gradient: dE[v] = scale·Σ_{tokens[n] = v} dX[n], in the order of n so that the
 // same call gives the same bits: no atomics on sums.
@@ -56,7 +55,7 @@ __device__ __forceinline__ void store_piece(E* row, int64_t c, int64_t C, const 
     }
 }
 
-constexpr int64_t STREAM_BYTES = (int64_t)32 << 20;
+constexpr int64_t L2_BYTES = (int64_t)32 << 20, INFINITY_CACHE_BYTES = (int64_t)256 << 20;
 
 template <typename E, bool STREAM>
 __global__ __launch_bounds__(256) void embedding_kernel(const int64_t* __restrict__ tokens, const E* __restrict__ table,
@@ -398,7 +397,10 @@ hipError_t launch_backward(const int64_t* tokens, const E* dX, int64_t lddx, E* 
     const int64_t zeros = accumulate ? 0 : (V + RUN_MOST - 1) / RUN_MOST;
     const unsigned chunks = (unsigned)((K + per_row * W - 1) / (per_row * W));
     const dim3 grid((unsigned)(runs + zeros), chunks);
-    if (V * K * (int64_t)sizeof(E) > STREAM_BYTES)
+    // Zero rows go past the caches where dE and dX do not fit the last one.  4096 tokens of
+    // a text on 32000 x 4096 73.5 -> 60 us, random ones on 50000 x 4096 100 -> 81; but 34
+    // tokens on 25480 x 3584 32 -> 44.
+    if ((V + N) * K * (int64_t)sizeof(E) > INFINITY_CACHE_BYTES)
         hipLaunchKernelGGL((reduce_runs_kernel<E, true>), grid, dim3(256), 0, stream, tokens, dX, lddx, dE, ldde, K,
                            (int)V, scale, accumulate ? 1 : 0, order, start, part, b.ldpart, (int)runs, places, per_row);
     else
@@ -418,7 +420,7 @@ hipError_t launch_embedding(const int64_t* tokens, const void* E, int64_t lde, v
     const int64_t total = N * ((K + (f32 ? 3 : 7)) / (f32 ? 4 : 8));
     const int64_t want = (total + 255) / 256;
     const dim3 grid((unsigned)(want < 65536 ? want : 65536)), block(256);
-    const bool past = N * K * (f32 ? 4 : 2) > STREAM_BYTES;
+    const bool past = N * K * (f32 ? 4 : 2) > L2_BYTES;
 #define LOOKUP(T, S)                                                                                              \
     hipLaunchKernelGGL((embedding_kernel<T, S>), grid, block, 0, stream, tokens, (const T*)E, lde, (T*)X, ldx, N, K, V, \
                        scale)

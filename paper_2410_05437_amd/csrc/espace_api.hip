@@ -768,21 +768,20 @@ GemmArgs f32_args(const void* A, int64_t lda, const void* B, int64_t ldb, void* 
 
 }  // namespace
 
-F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges, bool depth) {
-    const int64_t lim = (int64_t)1 << 31;
+static F32Plan make_f32_plan(int R, int Cc, int D, bool small, bool tiles, int ranges, bool depth, double extra) {
     const int cus = device_cus();
     const double byte_cost = 315.0 / (2.0 * 64 * cus);
     F32Plan p;
-    if (use_gemv((int)R, (int)Cc, (int)D)) {
+    if (use_gemv(R, Cc, D)) {
         p.kind = F32Plan::GEMV;
         return p;
     }
     double best = 1e300;
-    if (espace::mid_supported(lda, ldb)) {
+    if (small) {
         p.kind = F32Plan::MID;
-        best = espace::mid_plan((int)R, (int)Cc, (int)D, cus, ranges, &p.tile, &p.ranges);
+        best = espace::mid_plan(R, Cc, D, cus, ranges, &p.tile, &p.ranges) + extra;
     }
-    if (R * lda >= lim || Cc * ldb >= lim) return p;
+    if (!tiles) return p;
     const int ktiles = ceil_div(D, 64);
     for (const int bn : {256, 192})
         for (int s = 1; s <= ranges && (s == 1 || ktiles / s >= 8); ++s) {
@@ -796,6 +795,37 @@ F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int
             p.ranges = s;
         }
     return p;
+}
+
+// Each thread keeps the last plans it made, as plan_tn: a call asks for the same few
+// several times, and a search of many ranges takes some microseconds.
+F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges, bool depth, double extra) {
+    const int64_t lim = (int64_t)1 << 31;
+    const bool small = espace::mid_supported(lda, ldb), tiles = R * lda < lim && Cc * ldb < lim;
+    struct Entry {
+        int R = -1, Cc = 0, D = 0, cus = 0, ranges = 0, flags = 0;
+        double extra = 0;
+        F32Plan p;
+    };
+    struct Set { Entry e[4]; unsigned next = 0; };
+    static thread_local Set memo[16];
+    const int cus = device_cus(), flags = (small ? 1 : 0) | (tiles ? 2 : 0) | (depth ? 4 : 0);
+    const unsigned h = ((unsigned)R * 2654435761u) ^ ((unsigned)Cc * 2246822519u) ^ ((unsigned)D * 3266489917u);
+    Set& set = memo[(h >> 20) % 16];
+    for (const Entry& e : set.e)
+        if (e.R == R && e.Cc == Cc && e.D == D && e.cus == cus && e.ranges == ranges && e.flags == flags &&
+            e.extra == extra)
+            return e.p;
+    Entry& e = set.e[set.next++ % 4];
+    e.p = make_f32_plan((int)R, (int)Cc, (int)D, small, tiles, ranges, depth, extra);
+    e.R = (int)R;
+    e.Cc = (int)Cc;
+    e.D = (int)D;
+    e.cus = cus;
+    e.ranges = ranges;
+    e.flags = flags;
+    e.extra = extra;
+    return e.p;
 }
 
 espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,

@@ -49,7 +49,7 @@ constexpr int64_t kNarrow = 256;
 constexpr int64_t kTwoTerms = 128;
 // Depth ranges of the logits' and dX's products whose sums the next pass adds, and the
 // floats of them.
-constexpr int64_t kRanges = 16, kRangeFloats = (int64_t)1 << 24;
+constexpr int64_t kRanges = 32, kRangeFloats = (int64_t)1 << 24;
 
 int most_ranges(int64_t R, int64_t ld) { return (int)std::max<int64_t>(1, std::min(kRanges, kRangeFloats / (R * ld))); }
 
@@ -143,7 +143,9 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
         // (either operand order of dW's product has this price)
         const F32Plan w = f32_plan(K, b.P, depth, ldgt, ldgt, 1, true), small = f32_plan(b.P, K, depth, ldgt, ldgt, 1);
         b.w = w.kind == F32Plan::TILED ? way_of(w) : (small.kind == F32Plan::MID ? way_of(small) : Way{});
-        b.x = way_of(f32_plan(b.rows, K, b.P, b.ldp, b.ldp, b.ranges_x, true));
+        // (the small tiles take W transposed: read and written at 4.5 TB/s)
+        const double turned = 3.0 + 4e-6 * K * b.P / 4.5;
+        b.x = way_of(f32_plan(b.rows, K, b.P, b.ldp, b.ldp, b.ranges_x, true, turned));
         // two terms are added by the pass that rounds
         if (b.terms > 1 && b.x.how == Way::EPILOGUE) b.x.how = Way::RANGES;
         // the small tiles do not add to what is there, and the ranges of many pieces
