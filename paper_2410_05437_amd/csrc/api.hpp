@@ -65,9 +65,10 @@ struct F32Plan {
 F32Plan f32_plan(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, int ranges, bool depth = false,
                  double extra = 0);
 // The float32 sums of plan.ranges depth ranges on the tiles of a plan of kind TILED, with
-// B as [D][Cc]; *made of them, R·splitk_ld(Cc) apart.
+// B as [D][Cc]; *made of them, R·splitk_ld(Cc) apart.  count: the rows that there are
+// of R (a device int; NULL: all).
 espace_status run_tiled_ranges(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t R, int64_t Cc,
-                               int64_t D, int tile, int ranges, int* made, hipStream_t stream);
+                               int64_t D, int tile, int ranges, const int* count, int* made, hipStream_t stream);
 // C = scale[0]·A·Bᵀ rounded to bfloat16, on the small tiles of such a plan in one range.
 espace_status run_tn_scaled_mid(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
                                 int64_t R, int64_t Cc, int64_t D, int config, const float* scale, hipStream_t stream);

@@ -857,11 +857,12 @@ espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb,
 }
 
 espace_status run_tiled_ranges(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t R, int64_t Cc,
-                               int64_t D, int tile, int ranges, int* made, hipStream_t stream) {
+                               int64_t D, int tile, int ranges, const int* count, int* made, hipStream_t stream) {
     GemmArgs g = f32_args(A, lda, B, ldb, C, espace::splitk_ld((int)Cc), R, Cc, D);
     g.tile = tile;
     g.splits = ranges;
     g.b_depth = 1;
+    g.count = count;
     const hipError_t e = espace::launch_gemm_tn_bf16_v3_ranges(g, false, made, stream);
     if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
     return ESPACE_OK;

@@ -37,6 +37,7 @@ namespace espace {
 namespace {
 
 struct V3NoEpi {};
+struct V3Count { const int* count; };     // rows that there are of R
 
 // B as [Cc][D] (rows along the depth), or as [D][Cc]; SWAPPED: the latter, and C is
 // written transposed, [Cc][R].
@@ -275,6 +276,10 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
             const float a = epi.last ? epi.scale[0] : 1.f;
             const int c0 = col0 + 4 * lh;                            // of block j: + 16 j
             const int cl0 = col0 + 16 * (lh & 1) + 8 * (lh >> 1);    // of blocks 2 m, 2 m + 1: + 32 m
+            int to[V3_NB];
+            if (epi.rows && epi.last)
+#pragma unroll
+                for (int i = 0; i < V3_NB; ++i) to[i] = epi.rows[min(row0 + 16 * i + lr, R - 1)];
 #pragma unroll
             for (int i = 0; i < V3_NB; ++i) {
                 const int r = row0 + 16 * i + lr;
@@ -302,7 +307,7 @@ __device__ __forceinline__ void v3_loss_epilogue(const f32x4_t (&acc)[V3_NB][V3C
                     const u32x4_t v = pack(value(2 * m) * a, value(2 * m + 1) * a);
                     const int c = cl0 + 32 * m;
                     if (r >= R) continue;
-                    uint16_t* p = Cb + (int64_t)r * ldc + c;
+                    uint16_t* p = Cb + (int64_t)(epi.rows ? to[i] : r) * ldc + c;
                     if (c + 8 <= Cc) {
                         *reinterpret_cast<u32x4_t*>(p) = v;
                     } else if (c < Cc) {
@@ -355,6 +360,22 @@ void gemm_tn_bf16_v3_kernel(const uint16_t* __restrict__ A, int64_t lda,
     constexpr bool SPARE = MODE == V3_STATS || MODE == V3_GRAD;
     __shared__ __attribute__((aligned(16))) float spare[SPARE ? V3_NW * 16 * 128 : 1];
 
+    if constexpr (!std::is_same<EPI, V3NoEpi>::value)
+        if (MODE != V3_STATS && epi.count) {
+            // fewer rows, columns or depths than the launch is for
+            const int n = epi.count[0];
+            if (MODE == V3_GRAD) {
+                Cc = n;
+                tiles_c = (Cc + BN - 1) / BN;
+            } else if (BT == V3_B_SWAPPED) {
+                D = n;
+                ktiles_per_split = (D + V3_BK - 1) / V3_BK;
+            } else {
+                R = n;
+            }
+            ntiles = (R + V3_BM - 1) / V3_BM * tiles_c;
+            if ((int)blockIdx.x >= ntiles) return;
+        }
     const int ktiles = (D + V3_BK - 1) / V3_BK;
     const int kt0 = blockIdx.y * ktiles_per_split;
     const int kt_end = kt0 + ktiles_per_split < ktiles ? kt0 + ktiles_per_split : ktiles;
@@ -748,9 +769,10 @@ hipError_t launch_v3_ranges(const GemmArgs& g, bool upper, int* ranges, hipStrea
     *ranges = S;
     const int64_t ldp = splitk_ld(g.Cc);
     if (g.b_depth)
-        hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN, 0, V3NoEpi, V3_B_DEPTH>), dim3(ntiles, S),
+        hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN, 0, V3Count, V3_B_DEPTH>), dim3(ntiles, S),
                            dim3(V3_NW * 64), 0, stream, g.A, g.lda, g.B, g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D,
-                           tiles_c, ntiles, ktps, (int64_t)g.R * ldp, 0, nullptr, nullptr, 0ull, g.wait, 0, V3NoEpi{});
+                           tiles_c, ntiles, ktps, (int64_t)g.R * ldp, 0, nullptr, nullptr, 0ull, g.wait, 0,
+                           V3Count{g.count});
     else
         hipLaunchKernelGGL((gemm_tn_bf16_v3_kernel<V3_F32, BN>), dim3(ntiles, S), dim3(V3_NW * 64), 0, stream, g.A,
                            g.lda, g.B, g.ldb, (void*)g.partial, ldp, g.R, g.Cc, g.D, tiles_c, ntiles, ktps,

@@ -51,6 +51,7 @@ struct GemmArgs {
     int a_pairs = 0;    // A is in the row-pair layout (lda its pair pitch)
     int c_pairs = 0;    // write C (bf16) in the row-pair layout (ldc its pair pitch)
     int b_depth = 0;    // B is [D][Cc] (depth ranges of the four-wave kernel)
+    const int* count = nullptr;     // with b_depth: rows that there are of R (device)
     const float* scale = nullptr;   // small tiles in one range: C = scale[0] * sums, rounded
 };
 
@@ -131,6 +132,10 @@ struct LossEpi {
     int64_t ldacc = 0;
     const float* scale = nullptr;
     int add = 0, last = 0;
+    // the tokens are count[0] of those the launch is for (at least one): columns of grad,
+    // rows of grad_out (row i of C is then rows[i]), depth of grad_out_t
+    const int* count = nullptr;
+    const int* rows = nullptr;
 };
 enum LossMode { LOSS_STATS, LOSS_GRAD, LOSS_GRAD_OUT, LOSS_GRAD_OUT_T };
 // 256 x 256 and 256 x 192 plans (g.tile) with these epilogues.  hipErrorInvalidValue for

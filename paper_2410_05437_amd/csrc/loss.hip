@@ -296,30 +296,82 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ 
 
 // ---- backward ------------------------------------------------------------------
 
-// One workgroup: two passes over the tokens.
+// One workgroup: two passes over the tokens, COEF_OWN a thread kept in registers.
+constexpr int COEF_OWN = 8;
+
 __global__ __launch_bounds__(1024) void coef_kernel(const float* __restrict__ dloss,
                                                     const int64_t* __restrict__ labels,
                                                     const float* __restrict__ mass, float t, int N, int V,
-                                                    float* __restrict__ r, float* __restrict__ scale) {
+                                                    float* __restrict__ r, float* __restrict__ scale,
+                                                    const float* __restrict__ lse, LiveTokens live) {
     __shared__ float red[16];
+    __shared__ int found[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     auto coef = [&](int n) {
         if (labels) return labels[n] < 0 ? 0.f : (labels[n] >= V ? nan_f() : dloss[n]);
         return mass[n] == 0.f ? 0.f : dloss[n] * t;
     };
+    float own[COEF_OWN];
     float m = 0.f;
-    for (int n = threadIdx.x; n < N; n += 1024) {
+#pragma unroll
+    for (int u = 0; u < COEF_OWN; ++u) {
+        const int n = u * 1024 + threadIdx.x;
+        own[u] = n < N ? coef(n) : 0.f;
+        const float a = fabsf(own[u]);
+        if (a < INFINITY) m = fmaxf(m, a);
+    }
+    for (int n = COEF_OWN * 1024 + threadIdx.x; n < N; n += 1024) {
         const float a = fabsf(coef(n));
         if (a < INFINITY) m = fmaxf(m, a);
     }
     m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    if (lane == 0) red[wave] = m;
     __syncthreads();
     m = red[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) m = fmaxf(m, red[i]);
     if (m < 1.17549435e-38f) m = 1.f;             // all 0, or too small to divide by
-    for (int n = threadIdx.x; n < N; n += 1024) r[n] = coef(n) / m;
     if (threadIdx.x == 0) scale[0] = m;
+    int before = 0;                               // live tokens of the rounds before
+    auto round = [&](int n, float c) {
+        const float x = c / m;
+        if (n < N) r[n] = x;
+        if (!live.count) return;
+        const bool in = n < N && x != 0.f;
+        const unsigned long long mask = __ballot(in);
+        if (lane == 0) found[wave] = __popcll(mask);
+        __syncthreads();
+        int at = before + __popcll(mask & ((1ull << lane) - 1));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (i < wave) at += found[i];
+            before += found[i];
+        }
+        if (n < N) live.where[n] = in ? at : -1;
+        if (in) {
+            live.token[at] = n;
+            live.r[at] = x;
+            live.lse[at] = lse[n];
+            if (labels) live.labels[at] = labels[n];
+        }
+        __syncthreads();
+    };
+#pragma unroll
+    for (int u = 0; u < COEF_OWN; ++u)
+        if (u * 1024 < N) round(u * 1024 + threadIdx.x, own[u]);
+    for (int n0 = COEF_OWN * 1024; n0 < N; n0 += 1024) {
+        const int n = n0 + threadIdx.x;
+        round(n, n < N ? coef(n) : 0.f);
+    }
+    if (live.count && threadIdx.x == 0) {
+        live.count[0] = before > 0 ? before : 1;
+        if (before == 0) {
+            live.token[0] = 0;
+            live.r[0] = 0.f;
+            live.lse[0] = 0.f;
+            if (labels) live.labels[0] = -1;
+        }
+    }
 }
 
 __device__ __forceinline__ uint16_t to_elem(float v, uint16_t) { return (uint16_t)bf16_rne(v); }
@@ -409,12 +461,13 @@ __global__ __launch_bounds__(256) void fix_kernel(LossTargets t, const float* __
     const int n = (int)(at / t.T), j = (int)(at - (int64_t)n * t.T);
     const float rn = r[n];
     if (rn == 0.f) return;
+    const int row = out.where ? out.where[n] : n;
     float g = rn * (exp_f(picked[(int64_t)n * ldpk + j] - lse[n]) - t.p[at]);
     for (int term = 0; term < out.terms; ++term) {
         const E q = to_elem(g, E());
         g -= from_elem(q);
-        if (out.G) ((E*)out.G)[((int64_t)term * out.ldx + n) * out.ldg + c] = q;
-        if (out.GT) ((E*)out.GT)[c * out.ldgt + term * out.ldx + n] = q;
+        if (out.G) ((E*)out.G)[((int64_t)term * out.ldx + row) * out.ldg + c] = q;
+        if (out.GT) ((E*)out.GT)[c * out.ldgt + term * out.ldx + row] = q;
     }
 }
 
@@ -422,17 +475,24 @@ __global__ __launch_bounds__(256) void fix_kernel(LossTargets t, const float* __
 template <typename E>
 __global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict__ X, int64_t ldx_,
                                                              const float* __restrict__ r, int N, int K,
-                                                             E* __restrict__ dst, int64_t ldd, int64_t ldx, int terms) {
+                                                             E* __restrict__ dst, int64_t ldd, int64_t ldx, int terms,
+                                                             LiveTokens live) {
     constexpr int W = 16 / sizeof(E), PER = 64 / W;          // elements of a piece, pieces of 64
     __shared__ E tile[64][64 + 4 / sizeof(E)];
     const int n0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
+    if (live.count) {
+        N = live.count[0];
+        r = live.r;
+        if (n0 >= N) return;
+    }
 #pragma unroll
     for (int q = threadIdx.x; q < 64 * PER; q += 256) {
         const int n = n0 + q / PER, k = k0 + q % PER * W;
         struct { E v[W]; } x;
         u32x4_t raw = {0u, 0u, 0u, 0u};
         // rows of X are padded to 16 bytes
-        if (n < N && k < K && r[n] != 0.f) raw = *reinterpret_cast<const u32x4_t*>(X + (int64_t)n * ldx_ + k);
+        if (n < N && k < K && r[n] != 0.f)
+            raw = *reinterpret_cast<const u32x4_t*>(X + (int64_t)(live.count ? live.token[n] : n) * ldx_ + k);
         __builtin_memcpy(&x, &raw, 16);
 #pragma unroll
         for (int e = 0; e < W; ++e) tile[q / PER][q % PER * W + e] = x.v[e];
@@ -463,8 +523,10 @@ __global__ __launch_bounds__(256) void add_f32_kernel(f32x4_t* __restrict__ acc,
 template <typename E>
 __global__ __launch_bounds__(256) void sum_out_kernel(const float* __restrict__ src, int64_t lds, int slabs,
                                                       int64_t stride, const float* __restrict__ scale,
-                                                      E* __restrict__ out, int64_t ldo, int64_t R, int64_t C) {
+                                                      E* __restrict__ out, int64_t ldo, int64_t R, int64_t C, const int* __restrict__ count,
+                                                      const int* __restrict__ rows) {
     const float a = scale[0];
+    if (count) R = count[0];
     const int64_t pieces = (C + 7) / 8, total = R * pieces;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / pieces, c = (i - row * pieces) * 8;
@@ -481,7 +543,7 @@ __global__ __launch_bounds__(256) void sum_out_kernel(const float* __restrict__ 
             q.v[e] = to_elem(a * lo[e], E());
             q.v[4 + e] = to_elem(a * hi[e], E());
         }
-        E* o = out + row * ldo + c;
+        E* o = out + (count ? rows[row] : row) * ldo + c;
         if (c + 8 <= C) {
             u32x4_t raw[sizeof(E) / 2];
             __builtin_memcpy(raw, &q, 8 * sizeof(E));
@@ -491,6 +553,21 @@ __global__ __launch_bounds__(256) void sum_out_kernel(const float* __restrict__ 
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (c + e < C) o[e] = q.v[e];
+        }
+    }
+}
+
+// One wave per token.
+__global__ __launch_bounds__(256) void zero_dead_kernel(const float* __restrict__ r, uint16_t* __restrict__ out,
+                                                        int64_t ldo, int N, int64_t C) {
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (n >= N || r[n] != 0.f) return;
+    uint16_t* row = out + (int64_t)n * ldo;
+    for (int64_t c = (threadIdx.x & 63) * 8; c < C; c += 512) {
+        if (c + 8 <= C) {
+            *reinterpret_cast<u32x4_t*>(row + c) = u32x4_t{0u, 0u, 0u, 0u};
+        } else {
+            for (int e = 0; c + e < C; ++e) row[c + e] = 0;
         }
     }
 }
@@ -554,13 +631,13 @@ hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, floa
 }
 
 hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
-                            float* r, float* scale, hipStream_t stream) {
-    hipLaunchKernelGGL(coef_kernel, dim3(1), dim3(1024), 0, stream, dloss, labels, mass, t, N, V, r, scale);
+                            float* r, float* scale, const float* lse, const LiveTokens& live, hipStream_t stream) {
+    hipLaunchKernelGGL(coef_kernel, dim3(1), dim3(1024), 0, stream, dloss, labels, mass, t, N, V, r, scale, lse, live);
     return hipGetLastError();
 }
 
-// N < 2^22 tokens: at most 65536 workgroups of 64 rows in y
-static_assert((1 << 22) / 64 <= 65536, "launch limit");
+// N < 2^21 tokens: at most 32768 workgroups of 64 rows in y
+static_assert((1 << 21) / 64 <= 65535, "launch limit");
 
 hipError_t launch_loss_grad(const Logits& S, int N, int c0, int cols, float inv_t, const float* lse,
                             const float* r, const LossTargets& t, bool entries, const GradOut& out,
@@ -586,17 +663,18 @@ hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ld
 }
 
 hipError_t launch_transpose_live(const void* X, int64_t ldx_, const float* r, int N, int K, void* dst, int64_t ldd,
-                                 int64_t ldx, int terms, bool f32, hipStream_t stream) {
+                                 int64_t ldx, int terms, bool f32, const LiveTokens* live, hipStream_t stream) {
+    const LiveTokens l = live ? *live : LiveTokens{};
     // at most 65535 workgroups in y
     for (int k0 = 0; k0 < K; k0 += 65535 * 64) {
         const int k = K - k0 < 65535 * 64 ? K - k0 : 65535 * 64;
         const dim3 grid((N + 63) / 64, (k + 63) / 64), block(256);
         if (f32)
             hipLaunchKernelGGL(transpose_live_kernel<float>, grid, block, 0, stream, (const float*)X + k0, ldx_, r, N,
-                               k, (float*)dst + (int64_t)k0 * ldd, ldd, ldx, terms);
+                               k, (float*)dst + (int64_t)k0 * ldd, ldd, ldx, terms, l);
         else
             hipLaunchKernelGGL(transpose_live_kernel<uint16_t>, grid, block, 0, stream, (const uint16_t*)X + k0, ldx_,
-                               r, N, k, (uint16_t*)dst + (int64_t)k0 * ldd, ldd, ldx, terms);
+                               r, N, k, (uint16_t*)dst + (int64_t)k0 * ldd, ldd, ldx, terms, l);
     }
     return hipGetLastError();
 }
@@ -608,14 +686,20 @@ hipError_t launch_add_f32(float* acc, const float* src, int64_t elems, hipStream
 }
 
 hipError_t launch_sum_out(const float* src, int64_t lds, int slabs, int64_t stride, const float* scale, void* out,
-                          int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream) {
+                          int64_t ldo, int64_t R, int64_t C, bool f32, const LiveTokens* live, hipStream_t stream) {
     const dim3 grid(blocks_of(R * ((C + 7) / 8))), block(256);
+    const int *count = live ? live->count : nullptr, *rows = live ? live->token : nullptr;
     if (f32)
         hipLaunchKernelGGL(sum_out_kernel<float>, grid, block, 0, stream, src, lds, slabs, stride, scale, (float*)out,
-                           ldo, R, C);
+                           ldo, R, C, count, rows);
     else
         hipLaunchKernelGGL(sum_out_kernel<uint16_t>, grid, block, 0, stream, src, lds, slabs, stride, scale,
-                           (uint16_t*)out, ldo, R, C);
+                           (uint16_t*)out, ldo, R, C, count, rows);
+    return hipGetLastError();
+}
+
+hipError_t launch_zero_dead(const float* r, void* out, int64_t ldo, int N, int64_t C, hipStream_t stream) {
+    hipLaunchKernelGGL(zero_dead_kernel, dim3((N + 3) / 4), dim3(256), 0, stream, r, (uint16_t*)out, ldo, N, C);
     return hipGetLastError();
 }
 

@@ -63,10 +63,21 @@ hipError_t launch_loss_whole(const Logits& S, int N, int V, float temperature, c
 hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, float temperature, const LossTargets& t,
                               float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream);
 
+// The tokens with a gradient (r is not 0), in their order: count[0] of them (one with r
+// 0 where there is none), their numbers, and their r, lse and labels; where[n] the place
+// of token n among them, -1 of the others.
+struct LiveTokens {
+    int* count = nullptr;
+    int* token = nullptr;
+    int* where = nullptr;
+    float* r = nullptr;
+    float* lse = nullptr;
+    int64_t* labels = nullptr;
+};
 // r[n] = coef[n] / c and scale[0] = c, with coef the factor of token n's row of G (0
-// without a target) and c the largest of their magnitudes.
+// without a target) and c the largest of their magnitudes.  live.count NULL: not wanted.
 hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
-                            float* r, float* scale, hipStream_t stream);
+                            float* r, float* scale, const float* lse, const LiveTokens& live, hipStream_t stream);
 // A piece of G, N rows and `cols` columns, and its transpose (either NULL: not wanted).
 // terms 2: bfloat16 entries as a sum of two, the second ldx rows on in G and ldx columns
 // on in GT; rows and columns [N, ldx) of either are then zeros.
@@ -78,6 +89,7 @@ struct GradOut {
     int64_t ldx = 0;
     int terms = 1;
     bool f32 = false;
+    const int* where = nullptr;     // rows of live tokens alone
 };
 // G of columns [c0, c0 + cols) from their logits; entries: with those of a teacher,
 // else they are launch_loss_fix's.
@@ -89,13 +101,18 @@ hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ld
                            int N, int c0, int cols, const GradOut& out, hipStream_t stream);
 // dst[k][n] = X[n][k], 0 where r[n] is 0 and in the columns [N, ldx); terms 2: once
 // more ldx columns on.
+// live: dst[k][i] = X[token[i]][k] of the live tokens (terms 1; columns past them are
+// not all written).
 hipError_t launch_transpose_live(const void* X, int64_t ldx_, const float* r, int N, int K, void* dst, int64_t ldd,
-                                 int64_t ldx, int terms, bool f32, hipStream_t stream);
+                                 int64_t ldx, int terms, bool f32, const LiveTokens* live, hipStream_t stream);
 // acc += src (rows of ld elements, a multiple of 4)
 hipError_t launch_add_f32(float* acc, const float* src, int64_t elems, hipStream_t stream);
-// out[r][c] = scale[0]·Σ of `slabs` of src, `stride` apart, in their order
+// out[r][c] = scale[0]·Σ of `slabs` of src, `stride` apart, in their order; live: of the
+// live tokens' rows, to their rows of out
 hipError_t launch_sum_out(const float* src, int64_t lds, int slabs, int64_t stride, const float* scale, void* out,
-                          int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream);
+                          int64_t ldo, int64_t R, int64_t C, bool f32, const LiveTokens* live, hipStream_t stream);
+// zeros in the rows of the tokens without a gradient (r 0; bfloat16)
+hipError_t launch_zero_dead(const float* r, void* out, int64_t ldo, int N, int64_t C, hipStream_t stream);
 // zeros in the columns [0, C) of R rows
 hipError_t launch_zero(void* out, int64_t ldo, int64_t R, int64_t C, bool f32, hipStream_t stream);
 

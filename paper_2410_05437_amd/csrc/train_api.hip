@@ -73,7 +73,7 @@ Way way_of(const F32Plan& p) {
 
 struct Layout {
     size_t S, part, picked, col, p, logp, sorted, place, first;    // forward (S, col, p: both)
-    size_t mass, r, scale, XT, G, GT, WT, acc, out, total;         // backward
+    size_t mass, r, scale, XT, G, GT, WT, acc, out, live, total;   // backward
     int tile;                    // >= 0: the logits' epilogues on this tile
     int64_t P;                   // columns of a piece
     int terms;
@@ -136,6 +136,7 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
     if (T > 0) b.mass = take((size_t)N * 4);
     b.r = take((size_t)N * 4);
     b.scale = take(4);
+    b.live = take((size_t)N * 24 + 8);           // count, then LiveTokens' arrays
     const int64_t ldgt = b.ldn * b.terms, depth = b.terms == 1 ? N : ldgt;
     b.rows = depth;
     b.ranges_x = pieces <= 4 ? most_ranges(b.rows, b.ldk) : 1;
@@ -328,6 +329,18 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     const int64_t P = narrow ? std::min(V, kNarrow) : b.P;
     const int64_t pieces = (V + P - 1) / P;
     const Way wx = narrow ? Way{} : b.x, ww = narrow ? Way{} : b.w;
+    // the products of the tokens with a gradient alone, where all of them can (also where
+    // one is not wanted: the other has the same bits then)
+    const bool compact = fused && wx.tiled() && ww.tiled();
+    espace::LiveTokens live;
+    if (compact) {
+        live.labels = (int64_t*)(ws + b.live);
+        live.token = (int*)(live.labels + N);
+        live.where = live.token + N;
+        live.r = (float*)(live.where + N);
+        live.lse = live.r + N;
+        live.count = (int*)(live.lse + N);
+    }
     const int64_t slab = b.rows * b.ldk;                        // of dX's sums
     const bool many = pieces <= 4 && !narrow;                   // their ranges stay apart
     const int64_t ldgt = b.ldn * b.terms, ldwt = ld8(P);
@@ -337,10 +350,10 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     int sums = 0;                                               // slabs in acc
     log_plan(b, true, fused, N, K, V, t.labels ? 0 : t.T, P);
     ESPACE_LAUNCH("loss coefficients", espace::launch_loss_coef(dloss, t.labels, mass, temperature, (int)N, (int)V, r,
-                                                                scale, stream));
+                                                                scale, lse, live, stream));
     if (dW || fused)
         ESPACE_LAUNCH("transpose", espace::launch_transpose_live(X, ldx, r, (int)N, (int)K, XT, ldgt, b.ldn, b.terms,
-                                                                 f32, stream));
+                                                                 f32, compact ? &live : nullptr, stream));
     for (int64_t c0 = 0; c0 < V; c0 += P) {
         const int64_t cols = std::min(P, V - c0);
         const char* Wp = (const char*)W + (size_t)c0 * ldw * es;
@@ -353,13 +366,15 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         go.ldx = b.ldn;
         go.terms = b.terms;
         go.f32 = f32;
+        go.where = live.where;
         if (fused) {
             espace::LossEpi e;
             e.inv_t = inv_t;
             e.col0 = (int)c0;
-            e.labels = t.labels;
-            e.lse = lse;
-            e.r = r;
+            e.labels = t.labels ? (compact ? live.labels : t.labels) : nullptr;
+            e.lse = compact ? live.lse : lse;
+            e.r = compact ? live.r : r;
+            e.count = live.count;
             e.GT = (uint16_t*)go.GT;
             e.ldgt = ldgt;
             ESPACE_TRY(run_tn_loss(Wp, ldw, XT, ldgt, G, b.ldp, cols, N, K, b.tile, espace::LOSS_GRAD, e, stream));
@@ -382,12 +397,14 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
                 e.scale = scale;
                 e.add = c0 > 0;
                 e.last = last;
+                e.count = live.count;
+                e.rows = live.token;
                 ESPACE_TRY(run_tn_loss(G, b.ldp, Wp, ldw, dX, lddx, N, K, cols, wx.tile, espace::LOSS_GRAD_OUT, e,
                                        stream));
             } else if (wx.how == Way::RANGES) {
                 int made = 1;
                 ESPACE_TRY(run_tiled_ranges(G, b.ldp, Wp, ldw, acc + sums * slab, b.rows, K, cols, wx.tile, wx.ranges,
-                                            &made, stream));
+                                            live.count, &made, stream));
                 sums += made;
             } else if (wx.how == Way::SMALL) {
                 ESPACE_TRY(run_tn_scaled_mid(G, b.ldp, WT, ldwt, dX, lddx, N, K, cols, wx.tile, scale, stream));
@@ -406,20 +423,23 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
                 espace::LossEpi e;
                 e.scale = scale;
                 e.last = 1;
+                e.count = live.count;
                 ESPACE_TRY(run_tn_loss(XT, ldgt, G, b.ldp, o, lddw, K, cols, depth, ww.tile, espace::LOSS_GRAD_OUT_T, e,
                                        stream));
             } else if (ww.how == Way::SMALL) {
                 ESPACE_TRY(run_tn_scaled_mid(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ww.tile, scale, stream));
             } else {
                 ESPACE_TRY(run_tn_f32(GT, ldgt, XT, ldgt, out, b.ldk, cols, K, depth, dt, stream));
-                ESPACE_LAUNCH("gradient", espace::launch_sum_out(out, b.ldk, 1, 0, scale, o, lddw, cols, K, f32, stream));
+                ESPACE_LAUNCH("gradient", espace::launch_sum_out(out, b.ldk, 1, 0, scale, o, lddw, cols, K, f32, nullptr,
+                                                                 stream));
             }
         }
     }
     if (dX && (wx.how == Way::SUMS || wx.how == Way::RANGES))
         // a second term's rows are a slab of their own
         ESPACE_LAUNCH("gradient", espace::launch_sum_out(acc, b.ldk, sums * b.terms, slab / b.terms, scale, dX, lddx, N,
-                                                         K, f32, stream));
+                                                         K, f32, compact ? &live : nullptr, stream));
+    if (dX && compact) ESPACE_LAUNCH("gradient", espace::launch_zero_dead(r, dX, lddx, (int)N, K, stream));
     return ESPACE_OK;
 }
 

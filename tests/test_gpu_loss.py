@@ -404,3 +404,44 @@ def test_leading_dimensions_past_the_tiles_offsets(E, T):
     rX, bX, rW, bW = ref.grads(w, False)
     R.within(dX, rX, bX, "dX")
     R.within(dW, rW, bW, "dW")
+
+
+def _fused(capfd, call):
+    """(call(), whether each of its loss plans kept the logits in the tiles)."""
+    capfd.readouterr()
+    out = call()
+    return out, [line.split("fused=")[1][0] == "1" for line in capfd.readouterr().err.splitlines()
+                 if line.startswith("espace loss plan")]
+
+
+@pytest.mark.parametrize("T", [0, 5])
+@pytest.mark.parametrize("live", [0, 1, 191, 256, 257, 699, 700])
+def test_few_tokens_with_a_target(E, capfd, live, T):
+    """The tiles' products run over the tokens with a gradient alone."""
+    N, K, V, t = 700, 1032, 12345, 2.0 if T else 1.0
+    X, W, g = _head(N, K, V, BF16, seed=11)
+    some = torch.randperm(N, generator=g, device="cuda")[:live]
+    on = torch.zeros(N, dtype=torch.bool, device="cuda")
+    on[some] = True
+    X = R.padded(torch.where(on[:, None], X, float("nan")), BF16)
+    w = torch.where(on, _weight(N, g), float("inf"))
+    dX, dW = R.out(N, K, BF16, "cuda", extra=8), R.out(V, K, BF16, "cuda", extra=8)
+    clean = torch.where(on[:, None], X, 0.0).contiguous()
+    wc = torch.where(on, w, 0.0)
+    if T:
+        index, logits = _teacher(N, V, T, g)
+        index[~on] = -1
+        (loss, lse, picked), f1 = _fused(capfd, lambda: E.espace_linear_distillation(X, W, index, logits, t))
+        _, f2 = _fused(capfd, lambda: E.espace_linear_distillation_backward(w, X, W, index, logits, lse, picked, t, dX=dX, dW=dW))
+        ref = R.Loss(clean, W, index=index, logits=logits, t=t)
+    else:
+        labels = torch.where(on, torch.randint(0, V, (N,), generator=g, device="cuda"), -1)
+        (loss, lse), f1 = _fused(capfd, lambda: E.espace_linear_cross_entropy(X, W, labels))
+        _, f2 = _fused(capfd, lambda: E.espace_linear_cross_entropy_backward(w, X, W, labels, lse, dX=dX, dW=dW))
+        ref = R.Loss(clean, W, labels=labels)
+    assert f1 == [True] and f2 == [True]
+    R.within(loss, ref.loss, ref.dloss, "loss")
+    rX, bX, rW, bW = ref.grads(wc, False)
+    R.within(dX, rX, bX, "dX")
+    R.within(dW, rW, bW, "dW")
+    assert not dX[~on].any() and R.padding_untouched(dX) and R.padding_untouched(dW)
