@@ -251,26 +251,36 @@ __global__ __launch_bounds__(256) void stats_kernel(Logits S, int c0, int cols,
     }
 }
 
-// 16 tokens: 16 threads each join every 16th part of a token, in order; the wave's
-// lanes then take a token's entries.
-__global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ part, int nparts, int N, int V,
-                                                     float tt, LossTargets t, float* __restrict__ picked,
-                                                     int64_t ldpk, float* __restrict__ loss, float* __restrict__ lse) {
+// (m, l) of two sets together
+__device__ __forceinline__ void join(float& m, float& l, float m2, float l2) {
+    const float to = fmaxf(m, m2);
+    l = rescale(l, m, to) + rescale(l2, m2, to);
+    m = to;
+}
+
+// 16 tokens: 64 threads each join every 64th part of a token, in order, then each
+// other's; every wave takes a token's entries.
+__global__ __launch_bounds__(1024) void finish_kernel(const float2* __restrict__ part, int nparts, int N, int V,
+                                                      float tt, LossTargets t, float* __restrict__ picked,
+                                                      int64_t ldpk, float* __restrict__ loss, float* __restrict__ lse) {
     __shared__ float red_m[16][17], red_l[16][17], lse_of[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
     const int n = blockIdx.x * 16 + x;
     float m = -INFINITY, l = 0.f;
     if (n < N)
-        for (int i = y; i < nparts; i += 16) {
+        for (int i = y; i < nparts; i += 64) {
             const float2 q = part[(int64_t)i * N + n];
-            const float to = fmaxf(m, q.x);
-            l = rescale(l, m, to) + rescale(q.y, q.x, to);
-            m = to;
+            join(m, l, q.x, q.y);
         }
-    red_m[y][x] = m;
-    red_l[y][x] = l;
+    join(m, l, __shfl_xor(m, 16), __shfl_xor(l, 16));
+    join(m, l, __shfl_xor(m, 32), __shfl_xor(l, 32));
+    if (lane < 16) {
+        red_m[wave][x] = m;
+        red_l[wave][x] = l;
+    }
     __syncthreads();
-    if (y == 0) {
+    if (threadIdx.x < 16) {
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, red_m[i][x]);
@@ -286,12 +296,10 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ 
     }
     if (t.labels) return;
     __syncthreads();
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int k = wave; k < 16 && (int)blockIdx.x * 16 + k < N; k += 4) {
-        const int64_t row = (int64_t)blockIdx.x * 16 + k;
-        const float v = entries_loss(t, row, lane, lse_of[k], picked + row * ldpk, tt);
-        if (lane == 0) loss[row] = v;
-    }
+    const int64_t row = (int64_t)blockIdx.x * 16 + wave;
+    if (row >= N) return;
+    const float v = entries_loss(t, row, lane, lse_of[wave], picked + row * ldpk, tt);
+    if (lane == 0) loss[row] = v;
 }
 
 // ---- backward ------------------------------------------------------------------
@@ -625,7 +633,7 @@ hipError_t launch_loss_whole(const Logits& S, int N, int V, float temperature, c
 
 hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, float temperature, const LossTargets& t,
                               float* picked, int64_t ldpk, float* loss, float* lse, hipStream_t stream) {
-    hipLaunchKernelGGL(finish_kernel, dim3((N + 15) / 16), dim3(256), 0, stream, part, nparts, N, V,
+    hipLaunchKernelGGL(finish_kernel, dim3((N + 15) / 16), dim3(1024), 0, stream, part, nparts, N, V,
                        temperature * temperature, t, picked, ldpk, loss, lse);
     return hipGetLastError();
 }
