@@ -64,14 +64,7 @@ constexpr int TK = 32;                            // depth step: 128-byte rows
 template <int BM, int BN>
 __global__ __launch_bounds__(256, 2)
 void gemm_tn_f32_mfma_kernel(const float* __restrict__ A, int64_t lda, const float* __restrict__ B, int64_t ldb,
-                             float* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c, int per_range,
-                             int64_t stride) {
-    // depth range blockIdx.y: per_range elements, a multiple of TK; its sums `stride` on
-    const int first = blockIdx.y * per_range;
-    A += first;
-    B += first;
-    C += blockIdx.y * stride;
-    D = min(D - first, per_range);
+                             float* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c) {
     constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
     constexpr int STAGE = (BM + BN) * TK * 4;
     constexpr int LPW = (BM + BN) / 8 / 4;        // 1 KB loads (8 rows) per wave and stage
@@ -183,6 +176,214 @@ void gemm_tn_f32_mfma_kernel(const float* __restrict__ A, int64_t lda, const flo
     }
 }
 
+// x as the sum of three bfloat16: each rounds what the ones before it leave, whose
+// differences float32 holds exactly.  8 values to three 16-byte chunks.
+__device__ __forceinline__ void split3(f32x4_t lo, f32x4_t hi, u32x4_t (&t)[3]) {
+    float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            t[s][q] = pack_bf16x2(x[2 * q], x[2 * q + 1]);
+            x[2 * q] -= __uint_as_float(t[s][q] << 16);
+            x[2 * q + 1] -= __uint_as_float(t[s][q] & 0xffff0000u);
+        }
+}
+
+// The same product on the bfloat16 matrix cores (the losses' products): with a = a0 + a1 +
+// a2 and b likewise, a0 b0 + a0 b1 + a1 b0 + a1 b1 + a0 b2 + a2 b0 leaves out a1 b2 + a2 b1
+// + a2 b2, at most 2^-23 of |a b| (each term at most 2^-8 of the one before it), as two
+// roundings of float32; the sums are float32.  601 x 1000 x 5003 tokens, features and
+// vocabulary: error of the losses and gradients 4.9e-7, with the fp32 MFMA 1.7e-6, of
+// which a sum takes 8 times as many.  (An infinity is not the sum of its terms: NaN.)
+//
+// Six products of 16 times the fp32 MFMA's rate: 2.7 times its peak; a step of a 128 x 128
+// tile is 1536 cycles of MFMA per SIMD.  Each element is split once, by the thread that
+// loads it (some 110 vector instructions a step and wave), and lies in LDS as three planes
+// of 64-byte rows.  The splits stand between the MFMA (mix()), the loads run two steps
+// ahead, and 8 waves give each SIMD two: 601 x 1000 x 5003 on 128 x 128 tiles with 4 waves
+// and the loads one step ahead 66 us, scheduled 56, 8 waves 51, all of the split between
+// the MFMA 44 (fp32 MFMA: 65); 1024 x 1024 x 8192 108 -> 91.  Bound by the issue of vector
+// instructions and MFMA, 44% of the matrix cores' cycles; a third LDS stage, which takes
+// the wait after the barrier away, 45 us.
+template <int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, 2)
+void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const float* __restrict__ B, int64_t ldb,
+                              float* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c, int per_range,
+                              int64_t stride) {
+    constexpr int WM = BM / WR, WN = BN / WC, TM = WM / 32, TN = WN / 32;
+    constexpr int PLANE = (BM + BN) * TK * 2, STAGE = 3 * PLANE;
+    constexpr int ROWS = 16 * WR * WC;            // rows that the threads' pieces of 8 elements are of
+    constexpr int NP = (BM + BN) / ROWS;          // pieces a thread and step
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+    // depth range blockIdx.y: per_range elements, a multiple of 2 TK; its sums `stride` on
+    const int first = blockIdx.y * per_range;
+    A += first;
+    B += first;
+    C += blockIdx.y * stride;
+    D = min(D - first, per_range);
+    int tile_r, tile_c;
+    tile_coords<4>(blockIdx.x, gridDim.x, tiles_c, 0, tile_r, tile_c);
+    const int row0 = tile_r * BM, col0 = tile_c * BN;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr0 = wave / WC * WM, wc0 = wave % WC * WN;
+
+    // descriptors over the tile's own rows, from this range's first element on (the
+    // launcher checks that these span less than 2^32 bytes); rows past the matrix repeat
+    // its last row
+    const int nr = min(BM, R - row0), nc = min(BN, Cc - col0);
+    const auto ra = __builtin_amdgcn_make_buffer_rsrc((void*)(A + (int64_t)row0 * lda), (short)0,
+                                                      (int)(uint32_t)(((uint64_t)nr * lda - first) * 4u), 0x00020000);
+    const auto rb = __builtin_amdgcn_make_buffer_rsrc((void*)(B + (int64_t)col0 * ldb), (short)0,
+                                                      (int)(uint32_t)(((uint64_t)nc * ldb - first) * 4u), 0x00020000);
+    // piece j: 8 elements of row ROWS j + threadIdx.x / 4
+    const int prow = threadIdx.x >> 2, pk = (threadIdx.x & 3) * 8;
+    unsigned off[NP];
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+        const bool isA = ROWS * j < BM;
+        const int rr = ROWS * j + prow - (isA ? 0 : BM);
+        const int g = isA ? min(rr, nr - 1) : min(rr, nc - 1);
+        off[j] = (unsigned)(((uint64_t)g * (isA ? lda : ldb) + pk) * 4u);
+    }
+    // chunk c of row r sits at chunk c ^ ((r >> 2) & 3): the 16 rows of 64 bytes that
+    // neighbouring lanes read fall on all banks
+    unsigned char* const put = smem + prow * (TK * 2) + ((threadIdx.x & 3) ^ ((prow >> 2) & 3)) * 16;
+    // the elements of two steps in flight
+    f32x4_t x[2][NP][2];
+    auto load = [&](int t, int j) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            // chunks at or past the depth are read past the descriptor: zeros
+            const int k = t * TK + pk + 4 * h;
+            const unsigned o = k < D ? off[j] + (unsigned)(t * TK + 4 * h) * 4u : 0xFFFFFFF0u;
+            x[t & 1][j][h] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ROWS * j < BM ? ra : rb,
+                                                                                               (int)o, 0, 0));
+        }
+    };
+    // the chunk that straddles the depth: its padding is not used
+    auto mask = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[t & 1][j][h][e] = t * TK + pk + 4 * h + e < D ? x[t & 1][j][h][e] : 0.f;
+    };
+    auto stage_in = [&](int t, int j) {
+        u32x4_t v[3];
+        split3(x[t & 1][j][0], x[t & 1][j][1], v);
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+            *reinterpret_cast<u32x4_t*>(put + (t & 1) * STAGE + p * PLANE + j * ROWS * TK * 2) = v[p];
+    };
+
+    f32x16_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+    const int lr = lane & 31, lh = lane >> 5, sw = (lr >> 2) & 3;
+    const int steps = (D + TK - 1) / TK;
+    bf16x8_t fa[2][TM][3], fb[2][TN][3];
+    auto read = [&](int t, int u) {
+        const unsigned char* pa = smem + (t & 1) * STAGE + (wr0 + lr) * (TK * 2);
+        const unsigned char* pb = smem + (t & 1) * STAGE + (BM + wc0 + lr) * (TK * 2);
+        const int c = ((2 * u + lh) ^ sw) * 16;
+#pragma unroll
+        for (const int p : {1, 0, 2}) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                fa[u][i][p] = *reinterpret_cast<const bf16x8_t*>(pa + p * PLANE + i * 32 * TK * 2 + c);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                fb[u][j][p] = *reinterpret_cast<const bf16x8_t*>(pb + p * PLANE + j * 32 * TK * 2 + c);
+        }
+    };
+    auto multiply = [&](int u) {
+        // the smallest first
+        constexpr int ta[6] = {1, 1, 0, 0, 2, 0}, tb[6] = {1, 0, 1, 0, 0, 2};
+#pragma unroll
+        for (int q = 0; q < 6; ++q)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[u][j][tb[q]], fa[u][i][ta[q]], acc[i][j], 0,
+                                                                        0, 0);
+    };
+#pragma unroll
+    for (int j = 0; j < NP; ++j) load(0, j);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) load(1, j);
+    if (TK > D) mask(0);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+        stage_in(0, j);
+        load(2, j);
+    }
+    constexpr int HALF = NP / 2;
+    // a slab's MFMA between the split of the half of a later step, and its reads
+    auto mix = [&]() {
+#pragma unroll
+        for (int q = 0; q < 6 * TM * TN; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                    // MFMA
+            __builtin_amdgcn_sched_group_barrier(0x002, 54 * (NP - HALF) / (6 * TM * TN) + 1, 0);    // VALU
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                    // LDS reads
+            __builtin_amdgcn_sched_group_barrier(0x220, 1, 0);                    // LDS writes, loads
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // step t, whose parity the caller knows
+    auto step = [&](int t) {
+        if ((t + 2) * TK > D) mask(t + 1);
+        // every wave has written its part of step t and is done reading the other stage
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        read(t, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(0);
+        read(t, 1);
+#pragma unroll
+        for (int j = 0; j < HALF; ++j) {
+            stage_in(t + 1, j);
+            load(t + 3, j);
+        }
+        mix();
+        multiply(1);
+#pragma unroll
+        for (int j = HALF; j < NP; ++j) {
+            stage_in(t + 1, j);
+            load(t + 3, j);
+        }
+        mix();
+        // (the loads stay where they are)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // pairs of steps: past the depth they add zeros
+    for (int t = 0; t < steps; t += 2) {
+        step(t);
+        step(t + 1);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int r = row0 + wr0 + 32 * i + lr;
+        if (r >= R) continue;
+        float* row = C + (int64_t)r * ldc;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                store4(row, col0 + wc0 + 32 * j + 8 * q + 4 * lh, Cc,
+                       f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+    }
+}
+
 // Products too small to fill the chip with tiles: one MI x MI block of the
 // output per workgroup, its W waves taking turns at the depth (UD consecutive
 // slabs of 256 / MI each, loaded straight to registers), the partial sums
@@ -254,7 +455,7 @@ hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64
     const int few = R < Cc ? R : Cc;
     auto tiled = [&](auto kernel, int t) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)tiles(t)), dim3(256), 0, stream, A, lda, B, ldb, C, ldc, R, Cc, D,
-                           (Cc + t - 1) / t, D, (int64_t)0);
+                           (Cc + t - 1) / t);
         return hipGetLastError();
     };
     // one launch unless its 512-thread workgroups were 2^32 threads, a launch's limit
@@ -298,10 +499,10 @@ hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64
     return split(gemm_tn_f32_split_kernel<16, 8, 4>, 16);
 }
 
-// Tiles of 128 or 64 and depth ranges by their estimated time: the matrix cores' 133
-// TFLOP/s on the tiles of the fullest CU, a launch and its ramp 8 us, and the sums
-// written and read again.  us with one range by the rules above -> with the cheapest:
-// 601 x 1000 x 5003 90 -> 61, 5003 x 1000 x 601 87 -> 70, 275 x 256 x 15712 112 -> 42.
+// Tiles of 128 or 64 on the bfloat16 matrix cores, and depth ranges, by their estimated
+// time: the tiles of the fullest CU at the rates that the two reach (215 and 150
+// TFLOP/s), a launch and its ramp 8 us, and the sums written and read again.  us on one
+// range -> on the cheapest: FIGURES
 hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B, int64_t ldb, float* C, int64_t ldc,
                                      int R, int Cc, int D, int cus, int ranges, int* made, hipStream_t stream) {
     *made = 1;
@@ -314,7 +515,7 @@ hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B
         const int64_t tiles = (int64_t)((R + t - 1) / t) * ((Cc + t - 1) / t);
         for (int s = 1; s <= ranges && (s == 1 || D / s >= 128); ++s) {
             const int64_t rounds = (tiles * s + cus - 1) / cus;
-            const double us = rounds * (2.0 * t * t * D / s) / (133e6 / 256) + 8.0 +
+            const double us = rounds * (2.0 * t * t * D / s) / ((t == 64 ? 150e6 : 215e6) / 256) + 8.0 +
                               (s > 1 ? 2.0 * s * R * (double)Cc * 4 / 4e6 : 0.0);
             if (us < best) {
                 best = us;
@@ -323,16 +524,16 @@ hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B
             }
         }
     }
-    const int per = ((D + *made - 1) / *made + TK - 1) / TK * TK;
+    const int per = ((D + *made - 1) / *made + 2 * TK - 1) / (2 * TK) * (2 * TK);
     *made = (D + per - 1) / per;
     const int64_t tr = (R + tile - 1) / tile, tc = (Cc + tile - 1) / tile;
     const dim3 grid((unsigned)(tr * tc), (unsigned)*made);
     if (tile == 128)
-        hipLaunchKernelGGL((gemm_tn_f32_mfma_kernel<128, 128>), grid, dim3(256), 0, stream, A, lda, B, ldb, C, ldc, R, Cc,
-                           D, (int)tc, per, (int64_t)R * ldc);
+        hipLaunchKernelGGL((gemm_tn_f32_terms_kernel<128, 128, 2, 4>), grid, dim3(512), 0, stream, A, lda, B, ldb, C,
+                           ldc, R, Cc, D, (int)tc, per, (int64_t)R * ldc);
     else
-        hipLaunchKernelGGL((gemm_tn_f32_mfma_kernel<64, 64>), grid, dim3(256), 0, stream, A, lda, B, ldb, C, ldc, R, Cc,
-                           D, (int)tc, per, (int64_t)R * ldc);
+        hipLaunchKernelGGL((gemm_tn_f32_terms_kernel<64, 64, 2, 2>), grid, dim3(256), 0, stream, A, lda, B, ldb, C,
+                           ldc, R, Cc, D, (int)tc, per, (int64_t)R * ldc);
     return hipGetLastError();
 }
 
