@@ -52,6 +52,11 @@ espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, voi
 espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t R,
                          int64_t Cc, int64_t D, espace_dtype dt, hipStream_t stream, int ranges = 1,
                          int* made = nullptr);
+// float32 with an operand depth-major and the result scaled, where
+// gemm_tn_f32_terms_supported().
+espace_status run_tn_f32_depth(const float* A, int64_t lda, bool a_depth, const float* B, int64_t ldb, bool b_depth,
+                               float* C, int64_t ldc, int64_t R, int64_t Cc, int64_t D, const float* scale, int ranges,
+                               int* made, hipStream_t stream);
 // Its plan for bfloat16: the cheapest of 256 x 256 and 256 x 192 tiles, priced as the
 // other tiled products, and the small tiles; one or two rows may take the streaming
 // kernel, matrices past the kernels' offsets one with 64-bit ones.

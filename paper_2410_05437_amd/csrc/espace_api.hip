@@ -836,7 +836,7 @@ espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb,
     *made = 1;
     if (dt == ESPACE_F32) {
         e = espace::launch_gemm_tn_f32_ranges((const float*)A, lda, (const float*)B, ldb, C, ldc, (int)R, (int)Cc,
-                                              (int)D, device_cus(), ranges, made, stream);
+                                              (int)D, device_cus(), ranges, made, false, false, nullptr, stream);
     } else {
         GemmArgs g = f32_args(A, lda, B, ldb, C, ldc, R, Cc, D);
         const F32Plan p = f32_plan(R, Cc, D, lda, ldb, ranges);
@@ -852,6 +852,15 @@ espace_status run_tn_f32(const void* A, int64_t lda, const void* B, int64_t ldb,
                 e = espace::launch_gemm_tn_bf16(g, stream);
         }
     }
+    if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
+    return ESPACE_OK;
+}
+
+espace_status run_tn_f32_depth(const float* A, int64_t lda, bool a_depth, const float* B, int64_t ldb, bool b_depth,
+                               float* C, int64_t ldc, int64_t R, int64_t Cc, int64_t D, const float* scale, int ranges,
+                               int* made, hipStream_t stream) {
+    const hipError_t e = espace::launch_gemm_tn_f32_ranges(A, lda, B, ldb, C, ldc, (int)R, (int)Cc, (int)D, device_cus(),
+                                                           ranges, made, a_depth, b_depth, scale, stream);
     if (e != hipSuccess) return fail(ESPACE_ERR_HIP, "kernel launch: %s", hipGetErrorString(e));
     return ESPACE_OK;
 }

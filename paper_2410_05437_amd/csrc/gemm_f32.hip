@@ -9,6 +9,8 @@
 // to lane group q, and MFMA e of a slab takes element e of every chunk.  The
 // sums of 32 (tiled) or 8 to 16 terms are formed apart and then added, so that
 // a long sum rounds at its full size that many times less often.
+#include <type_traits>
+
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -206,11 +208,16 @@ __device__ __forceinline__ void split3(f32x4_t lo, f32x4_t hi, u32x4_t (&t)[3]) 
 // the MFMA 44 (fp32 MFMA: 65); 1024 x 1024 x 8192 108 -> 91.  Bound by the issue of vector
 // instructions and MFMA, 44% of the matrix cores' cycles; a third LDS stage, which takes
 // the wait after the barrier away, 45 us.
-template <int BM, int BN, int WR, int WC>
+//
+// AD, BD: the operand lies depth-major, [D][rows]: a thread's 8 elements are of as many
+// lines, which the lanes of a wave read along.  dX = G W and dW = G' X take W and G so,
+// without a pass that transposes either, and the result times `scale`: a step of 601 x
+// 1000 x 5003 228 -> 207 us, 100 x 2000 x 16000 357 -> 260.
+template <int BM, int BN, int WR, int WC, bool AD, bool BD>
 __global__ __launch_bounds__(64 * WR * WC, 2)
 void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const float* __restrict__ B, int64_t ldb,
                               float* __restrict__ C, int64_t ldc, int R, int Cc, int D, int tiles_c, int per_range,
-                              int64_t stride) {
+                              int64_t stride, const float* __restrict__ scale) {
     constexpr int WM = BM / WR, WN = BN / WC, TM = WM / 32, TN = WN / 32;
     constexpr int PLANE = (BM + BN) * TK * 2, STAGE = 3 * PLANE;
     constexpr int ROWS = 16 * WR * WC;            // rows that the threads' pieces of 8 elements are of
@@ -218,8 +225,8 @@ void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const fl
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
     // depth range blockIdx.y: per_range elements, a multiple of 2 TK; its sums `stride` on
     const int first = blockIdx.y * per_range;
-    A += first;
-    B += first;
+    A += first * (AD ? lda : 1);
+    B += first * (BD ? ldb : 1);
     C += blockIdx.y * stride;
     D = min(D - first, per_range);
     int tile_r, tile_c;
@@ -233,51 +240,69 @@ void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const fl
     // launcher checks that these span less than 2^32 bytes); rows past the matrix repeat
     // its last row
     const int nr = min(BM, R - row0), nc = min(BN, Cc - col0);
-    const auto ra = __builtin_amdgcn_make_buffer_rsrc((void*)(A + (int64_t)row0 * lda), (short)0,
-                                                      (int)(uint32_t)(((uint64_t)nr * lda - first) * 4u), 0x00020000);
-    const auto rb = __builtin_amdgcn_make_buffer_rsrc((void*)(B + (int64_t)col0 * ldb), (short)0,
-                                                      (int)(uint32_t)(((uint64_t)nc * ldb - first) * 4u), 0x00020000);
-    // piece j: 8 elements of row ROWS j + threadIdx.x / 4
-    const int prow = threadIdx.x >> 2, pk = (threadIdx.x & 3) * 8;
+    auto rsrc = [&](bool depth, const float* M, int64_t ld, int r0, int n) {
+        const uint64_t elems = depth ? (uint64_t)(D - 1) * ld + n : (uint64_t)n * ld - first;
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(M + (depth ? r0 : r0 * ld)), (short)0,
+                                                 (int)(uint32_t)(elems * 4u), 0x00020000);
+    };
+    const auto ra = rsrc(AD, A, lda, row0, nr), rb = rsrc(BD, B, ldb, col0, nc);
+    // piece j: 8 elements of row ROWS j + threadIdx.x / 4, or threadIdx.x % ROWS where the
+    // operand is depth-major; chunk c of row r sits at chunk c ^ ((r >> 2) & 3): the 16 rows
+    // of 64 bytes that neighbouring lanes read fall on all banks
+    auto row_of = [&](bool depth) { return depth ? (int)threadIdx.x % ROWS : (int)threadIdx.x >> 2; };
+    auto chunk_of = [&](bool depth) { return depth ? wave * 64 / ROWS : (int)threadIdx.x & 3; };
     unsigned off[NP];
+    int put[NP];
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const bool isA = ROWS * j < BM;
-        const int rr = ROWS * j + prow - (isA ? 0 : BM);
-        const int g = isA ? min(rr, nr - 1) : min(rr, nc - 1);
-        off[j] = (unsigned)(((uint64_t)g * (isA ? lda : ldb) + pk) * 4u);
+        const bool isA = ROWS * j < BM, dm = isA ? AD : BD;
+        const int64_t ld = isA ? lda : ldb;
+        const int rr = ROWS * j + row_of(dm), k = chunk_of(dm) * 8;
+        const int g = isA ? min(rr, nr - 1) : min(rr - BM, nc - 1);
+        off[j] = (unsigned)((uint64_t)(dm ? k * ld + g : g * ld + k) * 4u);
+        put[j] = rr * (TK * 2) + ((chunk_of(dm) ^ ((rr >> 2) & 3)) * 16);
     }
-    // chunk c of row r sits at chunk c ^ ((r >> 2) & 3): the 16 rows of 64 bytes that
-    // neighbouring lanes read fall on all banks
-    unsigned char* const put = smem + prow * (TK * 2) + ((threadIdx.x & 3) ^ ((prow >> 2) & 3)) * 16;
     // the elements of two steps in flight
     f32x4_t x[2][NP][2];
     auto load = [&](int t, int j) {
+        const bool isA = ROWS * j < BM;
+        if (isA ? AD : BD) {
+            // lines past the depth are past the descriptor: zeros (the launcher checks that
+            // those that are read ahead span less than 2^32 bytes, too)
+            const unsigned line = (unsigned)(isA ? lda : ldb) * 4u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[t & 1][j][e / 4][e % 4] = __builtin_bit_cast(
+                    float, __builtin_amdgcn_raw_buffer_load_b32(isA ? ra : rb, (int)(off[j] + (t * TK + e) * line), 0, 0));
+            return;
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             // chunks at or past the depth are read past the descriptor: zeros
-            const int k = t * TK + pk + 4 * h;
+            const int k = t * TK + chunk_of(false) * 8 + 4 * h;
             const unsigned o = k < D ? off[j] + (unsigned)(t * TK + 4 * h) * 4u : 0xFFFFFFF0u;
-            x[t & 1][j][h] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ROWS * j < BM ? ra : rb,
-                                                                                               (int)o, 0, 0));
+            x[t & 1][j][h] =
+                __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(isA ? ra : rb, (int)o, 0, 0));
         }
     };
     // the chunk that straddles the depth: its padding is not used
     auto mask = [&](int t) {
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
+        for (int j = 0; j < NP; ++j) {
+            if (ROWS * j < BM ? AD : BD) continue;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    x[t & 1][j][h][e] = t * TK + pk + 4 * h + e < D ? x[t & 1][j][h][e] : 0.f;
+                    x[t & 1][j][h][e] = t * TK + chunk_of(false) * 8 + 4 * h + e < D ? x[t & 1][j][h][e] : 0.f;
+        }
     };
     auto stage_in = [&](int t, int j) {
         u32x4_t v[3];
         split3(x[t & 1][j][0], x[t & 1][j][1], v);
 #pragma unroll
         for (int p = 0; p < 3; ++p)
-            *reinterpret_cast<u32x4_t*>(put + (t & 1) * STAGE + p * PLANE + j * ROWS * TK * 2) = v[p];
+            *reinterpret_cast<u32x4_t*>(smem + (t & 1) * STAGE + p * PLANE + put[j]) = v[p];
     };
 
     f32x16_t acc[TM][TN];
@@ -306,7 +331,7 @@ void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const fl
         }
     };
     auto multiply = [&](int u) {
-        // the smallest first
+        // in the order in which the terms are read
         constexpr int ta[6] = {1, 1, 0, 0, 2, 0}, tb[6] = {1, 0, 1, 0, 0, 2};
 #pragma unroll
         for (int q = 0; q < 6; ++q)
@@ -370,6 +395,7 @@ void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const fl
         step(t);
         step(t + 1);
     }
+    const float a = scale ? scale[0] : 1.f;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int r = row0 + wr0 + 32 * i + lr;
@@ -380,7 +406,8 @@ void gemm_tn_f32_terms_kernel(const float* __restrict__ A, int64_t lda, const fl
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 store4(row, col0 + wc0 + 32 * j + 8 * q + 4 * lh, Cc,
-                       f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+                       f32x4_t{a * acc[i][j][4 * q], a * acc[i][j][4 * q + 1], a * acc[i][j][4 * q + 2],
+                               a * acc[i][j][4 * q + 3]});
     }
 }
 
@@ -501,14 +528,24 @@ hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64
 
 // Tiles of 128 or 64 on the bfloat16 matrix cores, and depth ranges, by their estimated
 // time: the tiles of the fullest CU at the rates that the two reach (215 and 150
-// TFLOP/s), a launch and its ramp 8 us, and the sums written and read again.  us on one
-// range -> on the cheapest: FIGURES
+// TFLOP/s), a launch and its ramp 8 us, and the sums written and read again.  dX of N x K
+// x V on one range -> on the cheapest, us: 601 x 1000 x 5003 104 -> 47 (with the sums' pass
+// 52), 275 x 256 x 15712 291 -> 32, 100 x 2000 x 16000 298 -> 52.
+bool gemm_tn_f32_terms_supported(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, bool a_depth,
+                                 bool b_depth) {
+    // 32-bit byte offsets inside a tile, of the steps that are read ahead of the depth too
+    auto fits = [&](int64_t ld, bool depth) { return (depth ? D + 8 * TK : 128) * ld * 4 < ((int64_t)1 << 32); };
+    return R > 32 && Cc > 32 && fits(lda, a_depth) && fits(ldb, b_depth);
+}
+
 hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B, int64_t ldb, float* C, int64_t ldc,
-                                     int R, int Cc, int D, int cus, int ranges, int* made, hipStream_t stream) {
+                                     int R, int Cc, int D, int cus, int ranges, int* made, bool a_depth, bool b_depth,
+                                     const float* scale, hipStream_t stream) {
     *made = 1;
-    const bool fits = (lda > ldb ? lda : ldb) * 128 * 4 < ((int64_t)1 << 32);
-    if (!fits || (R < Cc ? R : Cc) <= 32)
+    if (!gemm_tn_f32_terms_supported(R, Cc, D, lda, ldb, a_depth, b_depth)) {
+        if (a_depth || b_depth || scale) return hipErrorInvalidValue;
         return launch_gemm_tn_f32(A, lda, B, ldb, C, ldc, R, Cc, D, cus, stream);
+    }
     double best = 1e300;
     int tile = 64;
     for (const int t : {64, 128}) {
@@ -528,13 +565,20 @@ hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B
     *made = (D + per - 1) / per;
     const int64_t tr = (R + tile - 1) / tile, tc = (Cc + tile - 1) / tile;
     const dim3 grid((unsigned)(tr * tc), (unsigned)*made);
-    if (tile == 128)
-        hipLaunchKernelGGL((gemm_tn_f32_terms_kernel<128, 128, 2, 4>), grid, dim3(512), 0, stream, A, lda, B, ldb, C,
-                           ldc, R, Cc, D, (int)tc, per, (int64_t)R * ldc);
-    else
-        hipLaunchKernelGGL((gemm_tn_f32_terms_kernel<64, 64, 2, 2>), grid, dim3(256), 0, stream, A, lda, B, ldb, C,
-                           ldc, R, Cc, D, (int)tc, per, (int64_t)R * ldc);
-    return hipGetLastError();
+    auto run = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, A, lda, B, ldb, C, ldc, R, Cc, D, (int)tc, per,
+                           (int64_t)R * ldc, scale);
+        return hipGetLastError();
+    };
+    auto order = [&](auto ad, auto bd) {
+        constexpr bool AD = decltype(ad)::value, BD = decltype(bd)::value;
+        return tile == 128 ? run(gemm_tn_f32_terms_kernel<128, 128, 2, 4, AD, BD>, 512)
+                           : run(gemm_tn_f32_terms_kernel<64, 64, 2, 2, AD, BD>, 256);
+    };
+    using No = std::false_type;
+    using Yes = std::true_type;
+    if (a_depth) return b_depth ? hipErrorInvalidValue : order(Yes{}, No{});
+    return b_depth ? order(No{}, Yes{}) : order(No{}, No{});
 }
 
 }  // namespace espace

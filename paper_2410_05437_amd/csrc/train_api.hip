@@ -78,6 +78,7 @@ struct Layout {
     int64_t P;                   // columns of a piece
     int terms;
     Way x, w;                    // dX's and dW's products
+    bool f32_x, f32_w;           // those of float32 read W, and G, as they lie
     int ranges_s, ranges_x;      // of the logits' (tile < 0) and dX's (sums) products, at most
     int64_t rows;                // of G, and of dX's sums: a second term's from ldn on
     int64_t ldn, ldp, ldk, ldfirst;
@@ -153,21 +154,23 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
         // find no room
         if ((b.x.how == Way::SMALL && (pieces > 1 || b.terms > 1)) || (b.x.how == Way::RANGES && pieces > 4)) b.x = Way{};
     }
+    b.f32_x = !bf16 && N > 32 && K > 32;
+    b.f32_w = !bf16 && espace::gemm_tn_f32_terms_supported(b.P, K, N, b.ldp, ldgt, true, false);
     // Narrow pieces, which take transposed operands and float32 sums, may be needed
     // where the tiles are planned.
-    const bool tiles = b.tile >= 0 || b.x.tiled();
+    const bool tiles = b.tile >= 0 || b.x.tiled() || b.f32_x;
     const int64_t narrow = ld8(std::min(V, kNarrow));
     b.XT = take((size_t)K * ldgt * es);
     b.G = take((size_t)b.rows * b.ldp * es);
-    b.GT = take((size_t)(b.w.tiled() ? narrow : b.P) * ldgt * es);
-    b.WT = take((size_t)K * (b.x.tiled() ? narrow : b.ldp) * es);
+    b.GT = take((size_t)(b.w.tiled() || b.f32_w ? narrow : b.P) * ldgt * es);
+    b.WT = take((size_t)K * (b.x.tiled() || b.f32_x ? narrow : b.ldp) * es);
     // sums of dX: of more than one piece to be added to, or ranges, or two pieces'
     int64_t sums = std::min<int64_t>(pieces, 2);
     if (b.x.how == Way::EPILOGUE || b.x.how == Way::SMALL) sums = pieces > 1 ? 1 : 0;
     else if (pieces <= 4) sums = b.ranges_x * pieces;
     if (tiles) sums = std::max<int64_t>(sums, 2);
     b.acc = take((size_t)b.rows * b.ldk * 4 * sums);
-    b.out = take((size_t)(b.w.how != Way::SUMS ? narrow : b.P) * b.ldk * 4);
+    b.out = take((size_t)(b.w.how != Way::SUMS || b.f32_w ? narrow : b.P) * b.ldk * 4);
     b.total = o;
     return b;
 }
@@ -324,7 +327,8 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     void *XT = ws + b.XT, *G = ws + b.G, *GT = ws + b.GT, *WT = ws + b.WT;
     const float inv_t = 1.f / temperature;
     // leading dimensions past the tiles' offsets: narrow pieces and float32 sums
-    const bool narrow = (b.tile >= 0 || b.x.tiled()) && (b.P * ldw >= kLim || K * b.ldn * b.terms >= kLim);
+    const bool narrow = ((b.tile >= 0 || b.x.tiled()) && (b.P * ldw >= kLim || K * b.ldn * b.terms >= kLim)) ||
+                        (b.f32_x && !espace::gemm_tn_f32_terms_supported(N, K, b.P, b.ldp, ldw, false, true));
     const bool fused = b.tile >= 0 && !narrow;
     const int64_t P = narrow ? std::min(V, kNarrow) : b.P;
     const int64_t pieces = (V + P - 1) / P;
@@ -358,10 +362,12 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
         const int64_t cols = std::min(P, V - c0);
         const char* Wp = (const char*)W + (size_t)c0 * ldw * es;
         const bool last = c0 + cols == V;
+        const bool fx = f32 && b.f32_x && !narrow;
+        const bool fw = f32 && espace::gemm_tn_f32_terms_supported(cols, K, N, b.ldp, ldgt, true, false);
         espace::GradOut go;
-        go.G = dX || fused || ww.tiled() ? G : nullptr;
+        go.G = dX || fused || ww.tiled() || fw ? G : nullptr;
         go.ldg = b.ldp;
-        go.GT = dW && !ww.tiled() ? GT : nullptr;
+        go.GT = dW && !ww.tiled() && !fw ? GT : nullptr;
         go.ldgt = ldgt;
         go.ldx = b.ldn;
         go.terms = b.terms;
@@ -388,7 +394,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
                                                                        (int)cols, go, stream));
         if (dX) {
-            if (!wx.tiled())
+            if (!wx.tiled() && !fx)
                 ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, ldwt, f32, stream));
             if (wx.how == Way::EPILOGUE) {
                 espace::LossEpi e;
@@ -410,8 +416,13 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
                 ESPACE_TRY(run_tn_scaled_mid(G, b.ldp, WT, ldwt, dX, lddx, N, K, cols, wx.tile, scale, stream));
             } else {
                 int made = 1;
-                ESPACE_TRY(run_tn_f32(G, b.ldp, WT, ldwt, acc + sums * slab, b.ldk, b.rows, K, cols, dt, stream,
-                                      many ? b.ranges_x : 1, &made));
+                float* to = acc + sums * slab;
+                const int most = many ? b.ranges_x : 1;
+                if (fx)
+                    ESPACE_TRY(run_tn_f32_depth((const float*)G, b.ldp, false, (const float*)Wp, ldw, true, to, b.ldk, N,
+                                                K, cols, nullptr, most, &made, stream));
+                else
+                    ESPACE_TRY(run_tn_f32(G, b.ldp, WT, ldwt, to, b.ldk, b.rows, K, cols, dt, stream, most, &made));
                 if (many || !sums) sums += made;
                 else ESPACE_LAUNCH("sum", espace::launch_add_f32(acc, acc + slab, slab, stream));
             }
@@ -428,6 +439,10 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
                                        stream));
             } else if (ww.how == Way::SMALL) {
                 ESPACE_TRY(run_tn_scaled_mid(GT, ldgt, XT, ldgt, o, lddw, cols, K, depth, ww.tile, scale, stream));
+            } else if (fw) {
+                int made = 1;
+                ESPACE_TRY(run_tn_f32_depth((const float*)G, b.ldp, true, (const float*)XT, ldgt, false, (float*)o, lddw,
+                                            cols, K, N, scale, 1, &made, stream));
             } else {
                 ESPACE_TRY(run_tn_f32(GT, ldgt, XT, ldgt, out, b.ldk, cols, K, depth, dt, stream));
                 ESPACE_LAUNCH("gradient", espace::launch_sum_out(out, b.ldk, 1, 0, scale, o, lddw, cols, K, f32, nullptr,

@@ -445,3 +445,34 @@ def test_few_tokens_with_a_target(E, capfd, live, T):
     R.within(dX, rX, bX, "dX")
     R.within(dW, rW, bW, "dW")
     assert not dX[~on].any() and R.padding_untouched(dX) and R.padding_untouched(dW)
+
+
+@pytest.mark.parametrize("size", [(33, 33, 40000), (100, 250, 300), (100, 257, 2500), (450, 131, 75000),
+                                  (450, 131, 65556)],
+                         ids=lambda s: "N%d_K%d_V%d" % s)
+@pytest.mark.parametrize("apart", [False, True], ids=["packed", "far"])
+def test_float32_products_read_their_operands_as_they_lie(E, size, apart):
+    """Pieces of the vocabulary whose last has few columns, tokens without a target that
+    hold NaN, and a head whose rows span 2^32 bytes and more: the same gradients."""
+    N, K, V = size
+    X, W, g = _head(N, K, V, F32, seed=12)
+    labels, w = _labels(N, V, g), _weight(N, g)
+    none = labels < 0
+    clean = torch.where(none[:, None], 0.0, X)
+    X = R.padded(torch.where(none[:, None], float("nan"), X), F32)
+    if apart:
+        ld = ((1 << 30) // V + 7) & ~3
+        far = torch.full((V * ld,), float("nan"), dtype=F32, device="cuda").as_strided((V, K), (ld, 1))
+        far.copy_(W)
+    else:
+        far = W
+    loss, lse = E.espace_linear_cross_entropy(X, far, labels)
+    dX, dW = R.out(N, K, F32, "cuda", extra=4), R.out(V, K, F32, "cuda", extra=4)
+    E.espace_linear_cross_entropy_backward(w, X, far, labels, lse, dX=dX, dW=dW)
+    ref = R.Loss(clean, W, labels=labels)
+    R.within(lse[~none, None], ref.lse[~none], ref.dlse[~none], "lse")
+    R.within(loss, ref.loss, ref.dloss, "loss")
+    rX, bX, rW, bW = ref.grads(w, False)
+    R.within(dX, rX, bX, "dX")
+    R.within(dW, rW, bW, "dW")
+    assert R.padding_untouched(dX) and R.padding_untouched(dW) and not dX[none].any()
