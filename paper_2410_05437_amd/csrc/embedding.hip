@@ -87,8 +87,9 @@ __global__ __launch_bounds__(256) void embedding_kernel(const int64_t* __restric
 
 constexpr int SORT_WAVES = 16;
 constexpr int SORT_BINS = 1024;           // entries per workgroup, at most
-constexpr int SORT_AHEAD = 8;             // groups of 64 tokens whose loads are in flight
 
+// AHEAD: groups of 64 tokens whose loads are in flight; a share of no more is read once.
+template <int AHEAD>
 __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int64_t* __restrict__ tokens, int N, int V,
                                                                       int bins, int bits, int* __restrict__ order,
                                                                       int* __restrict__ start) {
@@ -104,24 +105,28 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int6
     // this wave's share of the tokens, whole groups of 64
     const int groups = (N + 63) / 64, per = (groups + SORT_WAVES - 1) / SORT_WAVES;
     const int g0 = wave * per, g1 = g0 + per < groups ? g0 + per : groups;
-    // entries of SORT_AHEAD groups, relative to lo; -1 for a token outside the table or
-    // this wave's share
-    int64_t t[SORT_AHEAD];
+    // entries of AHEAD groups, relative to lo; -1 for a token outside the range or this
+    // wave's share
+    int rel[AHEAD];
+    int below = 0;
     auto load = [&](int g) {
+        int64_t t[AHEAD];
 #pragma unroll
-        for (int u = 0; u < SORT_AHEAD; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int n = (g + u) * 64 + lane;
             t[u] = g + u < g1 && n < N ? tokens[n] : -1;
         }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            below += t[u] >= 0 && t[u] < lo;
+            rel[u] = t[u] >= lo && t[u] < lo + nb ? (int)(t[u] - lo) : -1;
+        }
     };
-    int below = 0;
-    for (int g = g0; g < g1; g += SORT_AHEAD) {
+    for (int g = g0; g < g1; g += AHEAD) {
         load(g);
 #pragma unroll
-        for (int u = 0; u < SORT_AHEAD; ++u) {
-            if (t[u] >= 0 && t[u] < lo) ++below;
-            if (t[u] >= lo && t[u] < lo + nb) atomicAdd(&count[wave][(int)t[u] - lo], 1);
-        }
+        for (int u = 0; u < AHEAD; ++u)
+            if (rel[u] >= 0) atomicAdd(&count[wave][rel[u]], 1);
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) below += __shfl_xor(below, m);
@@ -156,14 +161,14 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int6
         }
     }
     __syncthreads();
-    for (int g = g0; g < g1; g += SORT_AHEAD) {
-        load(g);
+    for (int g = g0; g < g1; g += AHEAD) {
+        if (per > AHEAD) load(g);
 #pragma unroll
-        for (int u = 0; u < SORT_AHEAD; ++u) {
-            const bool in = t[u] >= lo && t[u] < lo + nb;
+        for (int u = 0; u < AHEAD; ++u) {
+            const bool in = rel[u] >= 0;
             unsigned long long same = __ballot(in);
             if (same == 0) continue;
-            const int bin = in ? (int)t[u] - lo : 0;
+            const int bin = in ? rel[u] : 0;
             // lanes with the same entry
             for (int bit = 0; bit < bits; ++bit) {
                 const unsigned long long on = __ballot((bin >> bit) & 1);
@@ -388,8 +393,16 @@ hipError_t launch_backward(const int64_t* tokens, const E* dX, int64_t lddx, E* 
     const int64_t bins = (V + 255) / 256 < SORT_BINS ? (V + 255) / 256 : SORT_BINS;
     int bits = 0;
     while (((int64_t)1 << bits) < bins) ++bits;
-    hipLaunchKernelGGL(sort_tokens_kernel, dim3((unsigned)((V + bins - 1) / bins)), dim3(SORT_WAVES * 64), 0, stream,
-                       tokens, (int)N, (int)V, (int)bins, bits, order, start);
+    const dim3 ranges((unsigned)((V + bins - 1) / bins)), threads(SORT_WAVES * 64);
+    // Shares of up to 8 groups of tokens, or 24, stay in registers between the two passes
+    // (read again -> kept: 8192 tokens 12.2 -> 10.5 us, 20011 19.0 -> 17.0); longer ones
+    // are read again, 8 groups at a time.
+    if (N > SORT_WAVES * 64 * 8 && N <= SORT_WAVES * 64 * 24)
+        hipLaunchKernelGGL(sort_tokens_kernel<24>, ranges, threads, 0, stream, tokens, (int)N, (int)V, (int)bins, bits,
+                           order, start);
+    else
+        hipLaunchKernelGGL(sort_tokens_kernel<8>, ranges, threads, 0, stream, tokens, (int)N, (int)V, (int)bins, bits,
+                           order, start);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int per_row = row_threads(K, W), groups = 256 / per_row, places = run_places(N, K, per_row, W);

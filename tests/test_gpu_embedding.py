@@ -54,7 +54,7 @@ def test_lookup(E, size, dtype, scale):
 
 
 GRAD = [(1, 1, 1), (1, 4096, 50), (63, 1003, 700), (64, 8, 3), (1000, 64, 5), (2049, 2056, 300), (4097, 260, 3000),
-        (3000, 24, 300001), (40000, 40, 1100)]
+        (3000, 24, 300001), (40000, 40, 1100), (8193, 40, 500), (20000, 132, 4096), (24576, 24, 1027)]
 
 
 @DT
