@@ -20,6 +20,10 @@
  * workspaces, statuses, streams; the same call on the same operands gives the same
  * bits again), with these additions: int64 and float32 arrays need their natural
  * alignment alone, a leading dimension of index, logits and picked any value >= T.
+ * float32 products of more than 32 rows and columns run on the bfloat16 matrix cores,
+ * a value as the sum of three bfloat16, to at most 2^-23 of each product beside the
+ * sums' roundings: an infinity, or a value that rounds to one in bfloat16, gives NaN
+ * there, and values below 2^-110 lose their last bits.
  * Limits: 1 <= V <= 2^30, 1 <= K <= 2^21, N < 2^21 (more tokens: several calls).
  *
  * Tokens without a target are part of the call and have no loss: it is 0, their row
@@ -54,8 +58,9 @@ espace_status espace_linear_cross_entropy(const void* X, int64_t ldx, const void
 /* Gradients for an upstream gradient dloss[n] = ∂ℓ/∂loss[n] (1/N for a mean):
  *     G[n][v] = dloss[n]·(exp(s_v - lse[n]) - [v = label])
  *     dX = G·W       dW = Gᵀ·X
- * bf16: G, taken relative to the largest |dloss|, is rounded to bfloat16 once; the
- * sums are float32 and rounded once (dX of several pieces: added in float32).
+ * bf16: G, taken relative to the largest |dloss|, is rounded to bfloat16 once (up to
+ * 128 tokens: kept as the sum of two bfloat16); the sums are float32 and rounded once
+ * (dX of several pieces: added in float32).
  * In: dloss [N], X, W, labels, lse [N] as the forward call gave it.  Out: dX [N][K]
  * (lddx) and/or dW [V][K] (lddw) (either may be NULL).
  * Needs espace_linear_loss_workspace_bytes(1, N, K, V, 0, dt). */
