@@ -163,11 +163,32 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int64_t* __restrict_
 
 // ---- forward -------------------------------------------------------------------
 
-// four logits, from the first slab's address
+// Q times four sums, from the first slab's address: the slabs are added in order, AHEAD
+// loads of each in flight (past the last: it again).
+template <int Q, int AHEAD>
+__device__ __forceinline__ void add_slabs(f32x4_t (&x)[Q], const float* p, int slabs, int64_t stride) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) x[q] = *reinterpret_cast<const f32x4_t*>(p + 4 * q);
+    for (int s = 1; s < slabs; s += AHEAD) {
+        f32x4_t y[AHEAD][Q];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                y[u][q] = *reinterpret_cast<const f32x4_t*>(p + min(s + u, slabs - 1) * stride + 4 * q);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (s + u < slabs)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) x[q] += y[u][q];
+    }
+}
+
+// four logits
 __device__ __forceinline__ f32x4_t logits4(const float* p, const Logits& S) {
-    f32x4_t x = *reinterpret_cast<const f32x4_t*>(p);
-    for (int s = 1; s < S.slabs; ++s) x += *reinterpret_cast<const f32x4_t*>(p + s * S.stride);
-    return x;
+    f32x4_t x[1];
+    add_slabs<1, 4>(x, p, S.slabs, S.stride);
+    return x[0];
 }
 
 // A token's loss from its targets' logits; all lanes of a wave, for an entry each.
@@ -540,16 +561,13 @@ __global__ __launch_bounds__(256) void sum_out_kernel(const float* __restrict__ 
         const int64_t row = i / pieces, c = (i - row * pieces) * 8;
         // rows of src are padded to a multiple of 8 columns
         const float* p = src + row * lds + c;
-        f32x4_t lo = *reinterpret_cast<const f32x4_t*>(p), hi = *reinterpret_cast<const f32x4_t*>(p + 4);
-        for (int s = 1; s < slabs; ++s) {
-            lo += *reinterpret_cast<const f32x4_t*>(p + s * stride);
-            hi += *reinterpret_cast<const f32x4_t*>(p + s * stride + 4);
-        }
+        f32x4_t x[2];
+        add_slabs<2, 8>(x, p, slabs, stride);
         struct { E v[8]; } q;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            q.v[e] = to_elem(a * lo[e], E());
-            q.v[4 + e] = to_elem(a * hi[e], E());
+            q.v[e] = to_elem(a * x[0][e], E());
+            q.v[4 + e] = to_elem(a * x[1][e], E());
         }
         E* o = out + (count ? rows[row] : row) * ldo + c;
         if (c + 8 <= C) {
