@@ -325,6 +325,16 @@ __global__ __launch_bounds__(1024) void finish_kernel(const float2* __restrict__
 
 // ---- backward ------------------------------------------------------------------
 
+__device__ __forceinline__ float coef_of(int n, const float* dloss, const int64_t* labels, const float* mass, float t,
+                                         int V) {
+    if (labels) return labels[n] < 0 ? 0.f : (labels[n] >= V ? nan_f() : dloss[n]);
+    return mass[n] == 0.f ? 0.f : dloss[n] * t;
+}
+// the largest of finite |a| that coefficients are taken relative to
+__device__ __forceinline__ float scale_of(float m) {
+    return m < 1.17549435e-38f ? 1.f : m;         // all 0, or too small to divide by
+}
+
 // One workgroup: two passes over the tokens, COEF_OWN a thread kept in registers.
 constexpr int COEF_OWN = 8;
 
@@ -336,10 +346,7 @@ __global__ __launch_bounds__(1024) void coef_kernel(const float* __restrict__ dl
     __shared__ float red[16];
     __shared__ int found[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    auto coef = [&](int n) {
-        if (labels) return labels[n] < 0 ? 0.f : (labels[n] >= V ? nan_f() : dloss[n]);
-        return mass[n] == 0.f ? 0.f : dloss[n] * t;
-    };
+    auto coef = [&](int n) { return coef_of(n, dloss, labels, mass, t, V); };
     float own[COEF_OWN];
     float m = 0.f;
 #pragma unroll
@@ -359,7 +366,7 @@ __global__ __launch_bounds__(1024) void coef_kernel(const float* __restrict__ dl
     m = red[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) m = fmaxf(m, red[i]);
-    if (m < 1.17549435e-38f) m = 1.f;             // all 0, or too small to divide by
+    m = scale_of(m);
     if (threadIdx.x == 0) scale[0] = m;
     int before = 0;                               // live tokens of the rounds before
     auto round = [&](int n, float c) {
@@ -500,28 +507,23 @@ __global__ __launch_bounds__(256) void fix_kernel(LossTargets t, const float* __
     }
 }
 
-// 64 x 64 through LDS, 16 bytes a load and a store.
-template <typename E>
-__global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict__ X, int64_t ldx_,
-                                                             const float* __restrict__ r, int N, int K,
-                                                             E* __restrict__ dst, int64_t ldd, int64_t ldx, int terms,
-                                                             LiveTokens live) {
+// 64 x 64 through LDS, 16 bytes a load and a store; from(n): the row of X that row n is,
+// -1 for zeros.
+template <typename E> using TransposeTile = E[64][64 + 4 / sizeof(E)];
+
+template <typename E, class From>
+__device__ __forceinline__ void transpose_tile(TransposeTile<E>& tile, const E* __restrict__ X, int64_t ldx_, int N,
+                                               int K, int n0, int k0, E* __restrict__ dst, int64_t ldd, int64_t ldx,
+                                               int terms, From from) {
     constexpr int W = 16 / sizeof(E), PER = 64 / W;          // elements of a piece, pieces of 64
-    __shared__ E tile[64][64 + 4 / sizeof(E)];
-    const int n0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
-    if (live.count) {
-        N = live.count[0];
-        r = live.r;
-        if (n0 >= N) return;
-    }
 #pragma unroll
     for (int q = threadIdx.x; q < 64 * PER; q += 256) {
         const int n = n0 + q / PER, k = k0 + q % PER * W;
         struct { E v[W]; } x;
         u32x4_t raw = {0u, 0u, 0u, 0u};
         // rows of X are padded to 16 bytes
-        if (n < N && k < K && r[n] != 0.f)
-            raw = *reinterpret_cast<const u32x4_t*>(X + (int64_t)(live.count ? live.token[n] : n) * ldx_ + k);
+        const int row = n < N && k < K ? from(n) : -1;
+        if (row >= 0) raw = *reinterpret_cast<const u32x4_t*>(X + (int64_t)row * ldx_ + k);
         __builtin_memcpy(&x, &raw, 16);
 #pragma unroll
         for (int e = 0; e < W; ++e) tile[q / PER][q % PER * W + e] = x.v[e];
@@ -540,6 +542,69 @@ __global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict
         for (int term = 0; term < terms; ++term)
             *reinterpret_cast<u32x4_t*>(dst + (int64_t)k * ldd + term * ldx + n) = raw;
     }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void transpose_live_kernel(const E* __restrict__ X, int64_t ldx_,
+                                                             const float* __restrict__ r, int N, int K,
+                                                             E* __restrict__ dst, int64_t ldd, int64_t ldx, int terms,
+                                                             LiveTokens live) {
+    __shared__ TransposeTile<E> tile;
+    const int n0 = blockIdx.x * 64;
+    if (live.count) {
+        N = live.count[0];
+        r = live.r;
+        if (n0 >= N) return;
+    }
+    transpose_tile<E>(tile, X, ldx_, N, K, n0, blockIdx.y * 64, dst, ldd, ldx, terms,
+                      [&](int n) { return r[n] == 0.f ? -1 : (live.count ? live.token[n] : n); });
+}
+
+// Few tokens: coef_kernel (workgroup 0) and the transposes of X and W in one launch; a
+// token is left out of X's where its coefficient is 0.
+constexpr int PREPARE_TOKENS = 2048;
+
+template <typename E>
+__global__ __launch_bounds__(256) void prepare_kernel(const float* __restrict__ dloss,
+                                                      const int64_t* __restrict__ labels,
+                                                      const float* __restrict__ mass, float t, int N, int V, int K,
+                                                      float* __restrict__ r, float* __restrict__ scale,
+                                                      const E* __restrict__ X, int64_t ldx_, E* __restrict__ XT,
+                                                      int64_t ldxt, int64_t ldn, int terms, int x_tiles,
+                                                      const E* __restrict__ W, int64_t ldw, E* __restrict__ WT,
+                                                      int64_t ldwt) {
+    auto coef = [&](int n) { return coef_of(n, dloss, labels, mass, t, V); };
+    if (blockIdx.x == 0) {
+        constexpr int OWN = PREPARE_TOKENS / 256;
+        __shared__ float red[4];
+        float own[OWN], m = 0.f;
+#pragma unroll
+        for (int u = 0; u < OWN; ++u) {
+            const int n = u * 256 + threadIdx.x;
+            own[u] = n < N ? coef(n) : 0.f;
+            const float a = fabsf(own[u]);
+            if (a < INFINITY) m = fmaxf(m, a);
+        }
+        m = wave_max(m);
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+        __syncthreads();
+        m = scale_of(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+        if (threadIdx.x == 0) scale[0] = m;
+#pragma unroll
+        for (int u = 0; u < OWN; ++u) {
+            const int n = u * 256 + threadIdx.x;
+            if (n < N) r[n] = own[u] / m;
+        }
+        return;
+    }
+    __shared__ TransposeTile<E> tile;
+    const int b = blockIdx.x - 1, across = (K + 63) / 64;
+    if (b < x_tiles)
+        transpose_tile<E>(tile, X, ldx_, N, K, b / across * 64, b % across * 64, XT, ldxt, ldn, terms,
+                          [&](int n) { return coef(n) == 0.f ? -1 : n; });
+    else
+        transpose_tile<E>(tile, W, ldw, V, K, (b - x_tiles) / across * 64, (b - x_tiles) % across * 64, WT, ldwt, ldwt,
+                          1, [](int v) { return v; });
 }
 
 __global__ __launch_bounds__(256) void add_f32_kernel(f32x4_t* __restrict__ acc, const f32x4_t* __restrict__ src,
@@ -659,6 +724,28 @@ hipError_t launch_loss_finish(const float2* part, int nparts, int N, int V, floa
 hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
                             float* r, float* scale, const float* lse, const LiveTokens& live, hipStream_t stream) {
     hipLaunchKernelGGL(coef_kernel, dim3(1), dim3(1024), 0, stream, dloss, labels, mass, t, N, V, r, scale, lse, live);
+    return hipGetLastError();
+}
+
+bool loss_prepare_supported(int64_t N, int64_t V, int64_t K) {
+    const int64_t across = (K + 63) / 64;
+    return N <= PREPARE_TOKENS && ((N + 63) / 64 + (V + 63) / 64) * across < (int64_t)1 << 23;
+}
+
+hipError_t launch_loss_prepare(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V, int K,
+                               float* r, float* scale, const void* X, int64_t ldx_, void* XT, int64_t ldxt, int64_t ldn,
+                               int terms, const void* W, int64_t ldw, void* WT, int64_t ldwt, bool f32,
+                               hipStream_t stream) {
+    const int across = (K + 63) / 64, x_tiles = XT ? (N + 63) / 64 * across : 0, w_tiles = WT ? (V + 63) / 64 * across : 0;
+    const dim3 grid(1 + x_tiles + w_tiles), block(256);
+    if (f32)
+        hipLaunchKernelGGL(prepare_kernel<float>, grid, block, 0, stream, dloss, labels, mass, t, N, V, K, r, scale,
+                           (const float*)X, ldx_, (float*)XT, ldxt, ldn, terms, x_tiles, (const float*)W, ldw,
+                           (float*)WT, ldwt);
+    else
+        hipLaunchKernelGGL(prepare_kernel<uint16_t>, grid, block, 0, stream, dloss, labels, mass, t, N, V, K, r, scale,
+                           (const uint16_t*)X, ldx_, (uint16_t*)XT, ldxt, ldn, terms, x_tiles, (const uint16_t*)W, ldw,
+                           (uint16_t*)WT, ldwt);
     return hipGetLastError();
 }
 

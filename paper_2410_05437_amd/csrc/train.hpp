@@ -76,6 +76,13 @@ struct LiveTokens {
 };
 // r[n] = coef[n] / c and scale[0] = c, with coef the factor of token n's row of G (0
 // without a target) and c the largest of their magnitudes.  live.count NULL: not wanted.
+// Coefficients, X transposed (XT null: not) and all of W (WT null: not) in one launch,
+// where supported and no list of live tokens is wanted.
+bool loss_prepare_supported(int64_t N, int64_t V, int64_t K);
+hipError_t launch_loss_prepare(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V, int K,
+                               float* r, float* scale, const void* X, int64_t ldx_, void* XT, int64_t ldxt, int64_t ldn,
+                               int terms, const void* W, int64_t ldw, void* WT, int64_t ldwt, bool f32,
+                               hipStream_t stream);
 hipError_t launch_loss_coef(const float* dloss, const int64_t* labels, const float* mass, float t, int N, int V,
                             float* r, float* scale, const float* lse, const LiveTokens& live, hipStream_t stream);
 // A piece of G, N rows and `cols` columns, and its transpose (either NULL: not wanted).

@@ -353,9 +353,18 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
     const bool few = !t.labels && !fused && t.T <= 64;
     int sums = 0;                                               // slabs in acc
     log_plan(b, true, fused, N, K, V, t.labels ? 0 : t.T, P);
-    ESPACE_LAUNCH("loss coefficients", espace::launch_loss_coef(dloss, t.labels, mass, temperature, (int)N, (int)V, r,
-                                                                scale, lse, live, stream));
-    if (dW || fused)
+    const bool turn_x = dW || fused, turn_w = dX && !wx.tiled() && !(f32 && b.f32_x && !narrow);
+    const bool together = !compact && espace::loss_prepare_supported(N, V, K);
+    const bool turned_w = together && turn_w && pieces == 1;
+    if (together)
+        ESPACE_LAUNCH("loss coefficients",
+                      espace::launch_loss_prepare(dloss, t.labels, mass, temperature, (int)N, (int)V, (int)K, r, scale,
+                                                  X, ldx, turn_x ? XT : nullptr, ldgt, b.ldn, b.terms, W, ldw,
+                                                  turned_w ? WT : nullptr, ldwt, f32, stream));
+    else
+        ESPACE_LAUNCH("loss coefficients", espace::launch_loss_coef(dloss, t.labels, mass, temperature, (int)N, (int)V,
+                                                                    r, scale, lse, live, stream));
+    if (turn_x && !together)
         ESPACE_LAUNCH("transpose", espace::launch_transpose_live(X, ldx, r, (int)N, (int)K, XT, ldgt, b.ldn, b.terms,
                                                                  f32, compact ? &live : nullptr, stream));
     for (int64_t c0 = 0; c0 < V; c0 += P) {
@@ -394,7 +403,7 @@ espace_status loss_backward(const void* X, int64_t ldx, const void* W, int64_t l
             ESPACE_LAUNCH("teacher's entries", espace::launch_loss_fix(t, picked, ldpk, lse, r, (int)N, (int)c0,
                                                                        (int)cols, go, stream));
         if (dX) {
-            if (!wx.tiled() && !fx)
+            if (turn_w && !turned_w)
                 ESPACE_LAUNCH("transpose", espace::launch_transpose(Wp, ldw, (int)cols, (int)K, WT, ldwt, f32, stream));
             if (wx.how == Way::EPILOGUE) {
                 espace::LossEpi e;
