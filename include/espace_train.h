@@ -20,10 +20,10 @@
  * workspaces, statuses, streams; the same call on the same operands gives the same
  * bits again), with these additions: int64 and float32 arrays need their natural
  * alignment alone, a leading dimension of index, logits and picked any value >= T.
- * float32 products of more than 32 rows and columns run on the bfloat16 matrix cores,
- * a value as the sum of three bfloat16, to at most 2^-23 of each product beside the
- * sums' roundings: an infinity, or a value that rounds to one in bfloat16, gives NaN
- * there, and values below 2^-110 lose their last bits.
+ * Most float32 products run on the bfloat16 matrix cores, a value as the sum of three
+ * bfloat16, to at most 2^-23 of each product beside the sums' roundings: an infinity, or
+ * a value that rounds to one in bfloat16, gives NaN there, and values below 2^-110 lose
+ * their last bits.
  * Limits: 1 <= V <= 2^30, 1 <= K <= 2^21, N < 2^21 (more tokens: several calls).
  *
  * Tokens without a target are part of the call and have no loss: it is 0, their row

@@ -533,9 +533,12 @@ hipError_t launch_gemm_tn_f32(const float* A, int64_t lda, const float* B, int64
 // 52), 275 x 256 x 15712 291 -> 32, 100 x 2000 x 16000 298 -> 52.
 bool gemm_tn_f32_terms_supported(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, bool a_depth,
                                  bool b_depth) {
-    // 32-bit byte offsets inside a tile, of the steps that are read ahead of the depth too
+    // 32-bit byte offsets inside a tile, of the steps that are read ahead of the depth too.
+    // Few rows leave most of a tile empty, but a depth-major B would have to be transposed
+    // first (dX of 16 x 2000 x 16000: the step 240 -> 167 us, 32 x 700 x 9000 87 -> 69, 28 x
+    // 432 x 3200 level).
     auto fits = [&](int64_t ld, bool depth) { return (depth ? D + 8 * TK : 128) * ld * 4 < ((int64_t)1 << 32); };
-    return R > 32 && Cc > 32 && fits(lda, a_depth) && fits(ldb, b_depth);
+    return (R > 32 || b_depth) && Cc > 32 && fits(lda, a_depth) && fits(ldb, b_depth);
 }
 
 hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B, int64_t ldb, float* C, int64_t ldc,

@@ -181,7 +181,7 @@ hipError_t launch_gemm_tn_f32_ranges(const float* A, int64_t lda, const float* B
                                      int R, int Cc, int D, int cus, int ranges, int* made, bool a_depth, bool b_depth,
                                      const float* scale, hipStream_t stream);
 // Whether it takes a depth-major operand ([D][R] or [D][Cc]; one of them) or a scale
-// (that of one range's result), which the kernels of few rows do not.
+// (that of one range's result), which the kernels of few rows or columns do not.
 bool gemm_tn_f32_terms_supported(int64_t R, int64_t Cc, int64_t D, int64_t lda, int64_t ldb, bool a_depth, bool b_depth);
 
 // fp32 sums of the depth ranges of a 256 x 256 or 256 x 192 tiled product

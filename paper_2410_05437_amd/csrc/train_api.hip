@@ -154,7 +154,7 @@ Layout loss_layout(bool backward, int64_t N, int64_t K, int64_t V, int64_t T, es
         // find no room
         if ((b.x.how == Way::SMALL && (pieces > 1 || b.terms > 1)) || (b.x.how == Way::RANGES && pieces > 4)) b.x = Way{};
     }
-    b.f32_x = !bf16 && N > 32 && K > 32;
+    b.f32_x = !bf16 && espace::gemm_tn_f32_terms_supported(N, K, b.P, b.ldp, K, false, true);
     b.f32_w = !bf16 && espace::gemm_tn_f32_terms_supported(b.P, K, N, b.ldp, ldgt, true, false);
     // Narrow pieces, which take transposed operands and float32 sums, may be needed
     // where the tiles are planned.

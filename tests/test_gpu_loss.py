@@ -447,7 +447,7 @@ def test_few_tokens_with_a_target(E, capfd, live, T):
     assert not dX[~on].any() and R.padding_untouched(dX) and R.padding_untouched(dW)
 
 
-@pytest.mark.parametrize("size", [(33, 33, 40000), (100, 250, 300), (100, 257, 2500), (450, 131, 75000),
+@pytest.mark.parametrize("size", [(1, 40, 3000), (16, 1999, 700), (33, 33, 40000), (100, 250, 300), (100, 257, 2500), (450, 131, 75000),
                                   (450, 131, 65556)],
                          ids=lambda s: "N%d_K%d_V%d" % s)
 @pytest.mark.parametrize("apart", [False, True], ids=["packed", "far"])
