@@ -18,6 +18,7 @@
 //    batch's padding) leaves a float32 partial row per block; further workgroups write
 //    the zeros of the entries without a token.
 //  * join: the partial rows of each such entry, added in order.
+// Up to 64 tokens need no sorting: few_tokens_kernel.
 #include <algorithm>
 
 #include "common.hpp"
@@ -192,12 +193,13 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_tokens_kernel(const int6
 // two) of 16 bytes each, workgroup y taking the per_row · W columns from y on; so
 // narrow rows leave room for several at a time.
 constexpr int RUN_MOST = 32;              // sorted places of a block of runs, at most
+constexpr int ZERO_GROUPS = 1 << 22;      // workgroups that write zeros, at most
 constexpr int ROWS_AHEAD = 8;             // rows whose loads are in flight
 
 // Sums of the runs in blocks of `places` sorted places, a block for every `per_row`
 // threads.  A run that goes on in the next block, or comes from the one before, leaves
 // its sum in the block's part 1, or 0 (one that does both: 0).  Workgroups from
-// run_groups on write the zeros of the entries without a token, RUN_MOST each.
+// run_groups on write the zeros of the entries without a token, RUN_MOST at a time.
 template <typename E, bool STREAM>
 __global__ __launch_bounds__(256) void reduce_runs_kernel(const int64_t* __restrict__ tokens,
                                                           const E* __restrict__ dX, int64_t lddx, E* __restrict__ dE,
@@ -209,18 +211,20 @@ __global__ __launch_bounds__(256) void reduce_runs_kernel(const int64_t* __restr
     const int group = threadIdx.x / per_row, groups = 256 / per_row;
     const int64_t c = ((int64_t)blockIdx.y * per_row + threadIdx.x % per_row) * W;
     if ((int)blockIdx.x >= run_groups) {
-        const int v0 = ((int)blockIdx.x - run_groups) * RUN_MOST;
         const int lane = threadIdx.x & 63;
-        // one bit an entry, in every wave
-        const int mine = v0 + (lane < RUN_MOST ? lane : RUN_MOST - 1);
-        const bool none = lane < RUN_MOST && mine < V && start[mine] == start[mine + 1];
-        const unsigned long long empty = __ballot(none);
         Piece<E> z;
 #pragma unroll
         for (int e = 0; e < W; ++e) z.v[e] = to_elem(0.f, E());
-        if (c < K)
-            for (int k = group; k < RUN_MOST; k += groups)
-                if ((empty >> k) & 1) store_piece<E, STREAM>(dE + (int64_t)(v0 + k) * ldde, c, K, z);
+        for (int64_t v0 = ((int)blockIdx.x - run_groups) * (int64_t)RUN_MOST; v0 < V;
+             v0 += ((int)gridDim.x - run_groups) * (int64_t)RUN_MOST) {
+            // one bit an entry, in every wave
+            const int64_t mine = v0 + (lane < RUN_MOST ? lane : RUN_MOST - 1);
+            const bool none = lane < RUN_MOST && mine < V && start[mine] == start[mine + 1];
+            const unsigned long long empty = __ballot(none);
+            if (c < K)
+                for (int k = group; k < RUN_MOST; k += groups)
+                    if ((empty >> k) & 1) store_piece<E, STREAM>(dE + (v0 + k) * ldde, c, K, z);
+        }
         return;
     }
     // rows of the workgroup's places, and the entries of those and their neighbours
@@ -343,6 +347,68 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_runs_kernel(const int64_t* 
     store_piece(out, c, K, o);
 }
 
+// A few tokens in one launch: a workgroup of RUN_MOST entries notes which tokens are of
+// each, one bit a token, writes the zeros of those without, and then each per_row threads
+// add an entry's rows in the tokens' order.
+constexpr int FEW_TOKENS = 64;
+
+template <typename E, bool STREAM>
+__global__ __launch_bounds__(256) void few_tokens_kernel(const int64_t* __restrict__ tokens, int N,
+                                                         const E* __restrict__ dX, int64_t lddx, E* __restrict__ dE,
+                                                         int64_t ldde, int64_t K, int V, float scale, int accumulate,
+                                                         int per_row) {
+    constexpr int W = Piece<E>::W;
+    static_assert(FEW_TOKENS == 64 && RUN_MOST <= 64, "a bit a token");
+    __shared__ unsigned long long of[RUN_MOST];
+    const int v0 = blockIdx.x * RUN_MOST, lane = threadIdx.x & 63;
+    if (threadIdx.x < RUN_MOST) of[threadIdx.x] = 0;
+    const int64_t t = (int)threadIdx.x < N ? tokens[threadIdx.x] : -1;
+    __syncthreads();
+    if (t >= v0 && t < v0 + RUN_MOST && t < V) atomicOr(&of[(int)t - v0], 1ull << threadIdx.x);
+    __syncthreads();
+    const int group = threadIdx.x / per_row, groups = 256 / per_row;
+    const int64_t c = ((int64_t)blockIdx.y * per_row + threadIdx.x % per_row) * W;
+    // one bit an entry, in every wave
+    const unsigned long long named = __ballot(lane < RUN_MOST && of[lane < RUN_MOST ? lane : 0] != 0);
+    if (c >= K) return;
+    if (!accumulate) {
+        Piece<E> z;
+#pragma unroll
+        for (int e = 0; e < W; ++e) z.v[e] = to_elem(0.f, E());
+        for (int k = group; k < RUN_MOST && v0 + k < V; k += groups)
+            if (!((named >> k) & 1)) store_piece<E, STREAM>(dE + (int64_t)(v0 + k) * ldde, c, K, z);
+    }
+    for (int k = group; k < RUN_MOST; k += groups) {
+        if (!((named >> k) & 1)) continue;
+        unsigned long long left = of[k];
+        E* out = dE + (int64_t)(v0 + k) * ldde;
+        float sum[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) sum[e] = 0.f;
+        while (left) {
+            Piece<E> x[ROWS_AHEAD];
+            bool there[ROWS_AHEAD];
+#pragma unroll
+            for (int u = 0; u < ROWS_AHEAD; ++u) {
+                there[u] = left != 0;
+                if (there[u]) x[u] = load_piece(dX + (int64_t)(__ffsll(left) - 1) * lddx + c);
+                left &= left - 1;
+            }
+#pragma unroll
+            for (int u = 0; u < ROWS_AHEAD; ++u)
+                if (there[u])
+#pragma unroll
+                    for (int e = 0; e < W; ++e) sum[e] += to_f32(x[u].v[e]);
+        }
+        Piece<E> o;
+        if (accumulate) o = load_piece(out + c);
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            o.v[e] = to_elem(accumulate ? to_f32(o.v[e]) + scale * sum[e] : scale * sum[e], E());
+        store_piece(out, c, K, o);
+    }
+}
+
 // Sorted places of a block: the most that leave 512 workgroups, two a CU.
 int run_places(int64_t N, int64_t K, int per_row, int W) {
     const int64_t chunks = (K + (int64_t)per_row * W - 1) / ((int64_t)per_row * W);
@@ -384,6 +450,26 @@ template <typename E>
 hipError_t launch_backward(const int64_t* tokens, const E* dX, int64_t lddx, E* dE, int64_t ldde, int64_t N, int64_t K,
                            int64_t V, float scale, bool accumulate, void* workspace, hipStream_t stream) {
     constexpr int W = Piece<E>::W;
+    const int per_row = row_threads(K, W), groups = 256 / per_row;
+    const unsigned chunks = (unsigned)((K + per_row * W - 1) / (per_row * W));
+    // Zero rows go past the caches where dE and dX do not fit the last one.  4096 tokens of
+    // a text on 32000 x 4096 73.5 -> 60 us, random ones on 50000 x 4096 100 -> 81; but 34
+    // tokens on 25480 x 3584 32 -> 44.
+    const bool stream_rows = (V + N) * K * (int64_t)sizeof(E) > INFINITY_CACHE_BYTES;
+    // One launch for a few tokens, three -> one, us (of text; all one entry): 64 x 128 on 500
+    // 16.3 -> 10.1 (16.7 -> 13.3), 16 x 4096 on 32000 40.9 -> 37.8 (42.7 -> 37.8), 64 x 8192 on
+    // 50000 172 -> 168 (173 -> 170); 128 tokens of one entry would take longer (17 -> 25).
+    // An accumulated gradient has to look at every entry of the table, so not of large ones.
+    if (N <= FEW_TOKENS && V <= (accumulate ? 1 << 17 : 1 << 25)) {
+        const dim3 grid((unsigned)((V + RUN_MOST - 1) / RUN_MOST), chunks);
+        if (stream_rows)
+            hipLaunchKernelGGL((few_tokens_kernel<E, true>), grid, dim3(256), 0, stream, tokens, (int)N, dX, lddx, dE,
+                               ldde, K, (int)V, scale, accumulate ? 1 : 0, per_row);
+        else
+            hipLaunchKernelGGL((few_tokens_kernel<E, false>), grid, dim3(256), 0, stream, tokens, (int)N, dX, lddx, dE,
+                               ldde, K, (int)V, scale, accumulate ? 1 : 0, per_row);
+        return hipGetLastError();
+    }
     const GradLayout b = grad_layout(N, K, V);
     char* ws = static_cast<char*>(workspace);
     int* order = (int*)(ws + b.order);
@@ -405,15 +491,12 @@ hipError_t launch_backward(const int64_t* tokens, const E* dX, int64_t lddx, E* 
                            order, start);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int per_row = row_threads(K, W), groups = 256 / per_row, places = run_places(N, K, per_row, W);
+    const int places = run_places(N, K, per_row, W);
     const int64_t blocks = (N + places - 1) / places, runs = (blocks + groups - 1) / groups;
-    const int64_t zeros = accumulate ? 0 : (V + RUN_MOST - 1) / RUN_MOST;
-    const unsigned chunks = (unsigned)((K + per_row * W - 1) / (per_row * W));
+    // (a launch has less than 2^32 threads)
+    const int64_t zeros = accumulate ? 0 : std::min<int64_t>((V + RUN_MOST - 1) / RUN_MOST, ZERO_GROUPS / chunks + 1);
     const dim3 grid((unsigned)(runs + zeros), chunks);
-    // Zero rows go past the caches where dE and dX do not fit the last one.  4096 tokens of
-    // a text on 32000 x 4096 73.5 -> 60 us, random ones on 50000 x 4096 100 -> 81; but 34
-    // tokens on 25480 x 3584 32 -> 44.
-    if ((V + N) * K * (int64_t)sizeof(E) > INFINITY_CACHE_BYTES)
+    if (stream_rows)
         hipLaunchKernelGGL((reduce_runs_kernel<E, true>), grid, dim3(256), 0, stream, tokens, dX, lddx, dE, ldde, K,
                            (int)V, scale, accumulate ? 1 : 0, order, start, part, b.ldpart, (int)runs, places, per_row);
     else

@@ -144,3 +144,30 @@ def test_captured(E, dtype):
         want = run((tokens * (k + 1) + k) % V)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+@DT
+@pytest.mark.parametrize("N", [5, 64, 65, 300])
+def test_gradient_of_the_largest_tables(E, dtype, N):
+    """More entries than a launch has threads for; few tokens and more."""
+    V, K = (1 << 29) + 7, 3
+    g = torch.Generator(device="cuda").manual_seed(N)
+    tokens = torch.randint(0, V, (N,), generator=g, device="cuda")
+    tokens[0], tokens[1], tokens[2], tokens[3] = V - 1, 0, V - 1, -1
+    dX = R.padded(torch.randn(N, K, generator=g, device="cuda").to(dtype), dtype)
+    dE = R.out(V, K, dtype, "cuda")
+    dE[:] = 1.0
+    E.espace_embedding_backward(tokens, dX, V, dE=dE)
+    named = tokens[tokens >= 0].unique()
+    at = torch.searchsorted(named, tokens.clamp(min=0))
+    ref, bound = R.embedding_grad(torch.where(tokens >= 0, at, -1), dX, named.numel(), 1.0)
+    R.within(dE[named], ref, bound, "dE")
+    dE[named] = 0.0
+    assert not bool(dE.any())
+    before = torch.randn(named.numel(), K, generator=g, device="cuda").to(dtype)
+    dE[named] = before
+    E.espace_embedding_backward(tokens, dX, V, dE=dE, accumulate=True)
+    ref, bound = R.embedding_grad(torch.where(tokens >= 0, at, -1), dX, named.numel(), 1.0, start=before)
+    R.within(dE[named], ref, bound, "dE")
+    dE[named] = 0.0
+    assert not bool(dE.any())

@@ -476,3 +476,21 @@ def test_float32_products_read_their_operands_as_they_lie(E, size, apart):
     R.within(dX, rX, bX, "dX")
     R.within(dW, rW, bW, "dW")
     assert R.padding_untouched(dX) and R.padding_untouched(dW) and not dX[none].any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 8, (1 << 25) + 5), (2, 8, (1 << 25) + 5), (40, 40, 1500001)],
+                         ids=lambda s: "N%d_K%d_V%d" % s)
+def test_large_vocabularies(E, size, dtype):
+    N, K, V = size
+    X, W, g = _head(N, K, V, dtype, seed=13)
+    labels, w = torch.randint(0, V, (N,), generator=g, device="cuda"), _weight(N, g)
+    labels[0] = V - 1
+    loss, lse = E.espace_linear_cross_entropy(X, W, labels)
+    dX, dW = E.espace_linear_cross_entropy_backward(w, X, W, labels, lse)
+    ref = R.Loss(X, W, labels=labels)
+    R.within(lse[:, None], ref.lse, ref.dlse, "lse")
+    R.within(loss, ref.loss, ref.dloss, "loss")
+    rX, bX, rW, bW = ref.grads(w, N <= 128)
+    R.within(dX, rX, bX, "dX")
+    R.within(dW, rW, bW, "dW")
