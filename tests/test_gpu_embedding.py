@@ -171,3 +171,17 @@ def test_gradient_of_the_largest_tables(E, dtype, N):
     R.within(dE[named], ref, bound, "dE")
     dE[named] = 0.0
     assert not bool(dE.any())
+
+
+@DT
+def test_most_tokens_a_call_takes(E, dtype):
+    N, K, V = (1 << 21) - 1, 16, 5000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    tokens = _tokens(N, V, "frequent", g)
+    table = R.padded(torch.randn(V, K, generator=g, device="cuda").to(dtype), dtype)
+    X = E.espace_embedding(tokens, table)
+    assert torch.equal(X, table[tokens])
+    dE = E.espace_embedding_backward(tokens, X, V)
+    # (on the CPU: many float64 atomics on one row take minutes)
+    ref, bound = R.embedding_grad(tokens.cpu(), X.cpu(), V, 1.0)
+    R.within(dE.cpu(), ref, bound, "dE")

@@ -494,3 +494,28 @@ def test_large_vocabularies(E, size, dtype):
     rX, bX, rW, bW = ref.grads(w, N <= 128)
     R.within(dX, rX, bX, "dX")
     R.within(dW, rW, bW, "dW")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T", [0, 3])
+def test_most_tokens_a_call_takes(E, dtype, T):
+    N, K, V, t = (1 << 21) - 1, 16, 130, 2.0 if T else 1.0
+    X, W, g = _head(N, K, V, dtype, seed=14)
+    w = _weight(N, g)
+    if T:
+        index = torch.randint(0, V, (N, T), generator=g, device="cuda")
+        logits = torch.randn(N, T, generator=g, device="cuda") * 3.0
+        loss, lse, picked = E.espace_linear_distillation(X, W, index, logits, t)
+        dX, dW = E.espace_linear_distillation_backward(w, X, W, index, logits, lse, picked, t)
+        ref = R.Loss(X, W, index=index, logits=logits, t=t)
+        R.within(picked, ref.picked, ref.dpicked, "picked")
+    else:
+        labels = _labels(N, V, g)
+        loss, lse = E.espace_linear_cross_entropy(X, W, labels)
+        dX, dW = E.espace_linear_cross_entropy_backward(w, X, W, labels, lse)
+        ref = R.Loss(X, W, labels=labels)
+    R.within(lse[:, None], ref.lse, ref.dlse, "lse")
+    R.within(loss, ref.loss, ref.dloss, "loss")
+    rX, bX, rW, bW = ref.grads(w, False)
+    R.within(dX, rX, bX, "dX")
+    R.within(dW, rW, bW, "dW")
