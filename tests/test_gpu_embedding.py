@@ -185,3 +185,17 @@ def test_most_tokens_a_call_takes(E, dtype):
     # (on the CPU: many float64 atomics on one row take minutes)
     ref, bound = R.embedding_grad(tokens.cpu(), X.cpu(), V, 1.0)
     R.within(dE.cpu(), ref, bound, "dE")
+
+
+@DT
+@pytest.mark.parametrize("N", [10, 100])
+def test_widest_rows(E, dtype, N):
+    K, V = 1 << 21, 23
+    g = torch.Generator(device="cuda").manual_seed(N)
+    tokens = _tokens(N, V, "frequent", g)
+    table = torch.randn(V, K, generator=g, device="cuda").to(dtype)
+    X = E.espace_embedding(tokens, table)
+    assert torch.equal(X, table[tokens])
+    dE = E.espace_embedding_backward(tokens, X, V)
+    ref, bound = R.embedding_grad(tokens.cpu(), X.cpu(), V, 1.0)
+    R.within(dE.cpu(), ref, bound, "dE")

@@ -519,3 +519,22 @@ def test_most_tokens_a_call_takes(E, dtype, T):
     rX, bX, rW, bW = ref.grads(w, False)
     R.within(dX, rX, bX, "dX")
     R.within(dW, rW, bW, "dW")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("N", [3, 140])
+def test_widest_rows(E, dtype, N):
+    K, V = 1 << 21, 40
+    X, W, g = _head(N, K, V, dtype, seed=15)
+    labels, w = _labels(N, V, g), _weight(N, g)
+    loss, lse = E.espace_linear_cross_entropy(X, W, labels)
+    dX, dW = E.espace_linear_cross_entropy_backward(w, X, W, labels, lse)
+    ref = R.Loss(X, W, labels=labels)
+    R.within(lse[:, None], ref.lse, ref.dlse, "lse")
+    R.within(loss, ref.loss, ref.dloss, "loss")
+    # beside the bound for roundings that all err one way, that of a random walk: sqrt(K)
+    # half steps of sums up to 8 are 7e-4
+    assert float((lse.double() - ref.lse[:, 0]).abs().max()) <= 1e-3
+    rX, bX, rW, bW = ref.grads(w, N <= 128)
+    R.within(dX, rX, bX, "dX")
+    R.within(dW, rW, bW, "dW")
