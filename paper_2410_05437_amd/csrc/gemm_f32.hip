@@ -1,8 +1,9 @@
 // float32 "TN" product C[r][c] = sum_k A[r][k] * B[c][k] on the fp32 MFMA
-// (the float32 layers and gradients, the calibration products).
+// (the float32 layers and gradients, the calibration products), and the losses'
+// products on the bfloat16 one (gemm_tn_f32_terms_kernel).
 //
 // fp32 MFMA issue 256 flops per clock and CU, twice the vector ALU's rate
-// without packed instructions.  In both kernels the MFMA takes the B rows as
+// without packed instructions.  In both kernels on them the MFMA takes the B rows as
 // its first operand, so a lane ends with runs of 4 consecutive output columns
 // of one row, and the depth index of an operand is permuted the same way for
 // both: a lane's 16-byte chunk holds 4 consecutive k, chunk q of a row goes
