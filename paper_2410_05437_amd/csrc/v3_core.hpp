@@ -154,8 +154,9 @@ __device__ __forceinline__ void v3_load(unsigned char* smem, const uint16_t* A, 
 // buffer_load ... lds (8 per wave, returns 8), the depth tail through
 // registers with the elements at or beyond D zeroed (returns 0: nothing of
 // it stays in flight).
-// BT: rows of B past the depth are read from past the buffer (zeros), before A's part:
-// A's loads, which the registers wait for, are the newer ones.
+// BT: rows of B past the depth are read from past the buffer (zeros), into LDS as those
+// of full depth, so this waits for them: A's loads are the newer ones, but a half-stage
+// that starts at the depth or past it has none.
 template <class C, bool APAIR = false, bool BT = false>
 __device__ __forceinline__ int v3_load_half(unsigned char* smem, const uint16_t* A, const uint16_t* B,
                                             unsigned a_bytes, unsigned b_bytes, const int* voff,
@@ -190,6 +191,7 @@ __device__ __forceinline__ int v3_load_half(unsigned char* smem, const uint16_t*
         const u32x4_t v = load_chunk_masked(rowp, k0 + lc * 8, D);
         *reinterpret_cast<u32x4_t*>(smem + u * C::HS + q * 1024 + lane * 16) = v;
     }
+    if constexpr (BT) v3_wait_vm<0>();
     return 0;
 }
 
