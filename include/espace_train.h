@@ -28,9 +28,15 @@
  *
  * Tokens without a target are part of the call and have no loss: it is 0, their row
  * of dX is 0, and they add nothing to dW, whatever their rows of X and their dloss
- * hold (NaN and infinities included).  Targets outside the vocabulary (>= V) are a
- * caller's error that only the device sees: they give NaN in that token's loss and
- * row of dX, and in a row of dW.
+ * hold (NaN and infinities included).
+ *
+ * Targets outside the vocabulary (>= V) are a caller's error that only the device
+ * sees.  The token's loss is NaN, and so are, of the gradients,
+ *     a label             the token's row of dX and every row of dW
+ *     a teacher's entry   the token's row of dX and the rows of dW of all its entries,
+ *                         where the last one, V - 1, stands for those past the
+ *                         vocabulary (none of them where the token's dloss is 0)
+ * lse, the other tokens' losses and rows of dX, and the other rows of dW are right.
  */
 #ifndef ESPACE_TRAIN_H
 #define ESPACE_TRAIN_H
