@@ -39,13 +39,8 @@ espace_status check_alias(const Range& out, const Range* ins, int n);
 espace_status check_workspace(void* ws, size_t have, size_t need);
 espace_status check_device();
 
-// C[r][c] = Σ_k A[r][k]·B[c][k], C of type dt, under the library's plan for the sizes;
-// `partial`: run_tn_partial_bytes of scratch.
-size_t run_tn_partial_bytes(int64_t R, int64_t Cc, int64_t D, espace_dtype dt);
-espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R,
-                     int64_t Cc, int64_t D, espace_dtype dt, void* partial, hipStream_t stream);
-
-// The same with C in float32 whatever the operands' type, ldc = splitk_ld(Cc) and C
+// C[r][c] = Σ_k A[r][k]·B[c][k] under the library's plan for the sizes, with C in float32
+// whatever the operands' type, ldc = splitk_ld(Cc) and C
 // the library's own scratch: columns up to ldc may be written.  Needs no partial
 // sums.  ranges > 1: the sums of up to so many depth ranges, *made of them, R·ldc apart
 // in C, not combined.

@@ -740,10 +740,6 @@ espace_status run_tn(const void* A, int64_t lda, const void* B, int64_t ldb, voi
     return run_tn(A, lda, B, ldb, C, ldc, R, Cc, D, dt, partial, stream, 0, 0, kMaxRanges);
 }
 
-size_t run_tn_partial_bytes(int64_t R, int64_t Cc, int64_t D, espace_dtype dt) {
-    return plan_tn(R, Cc, D, dt).partial_bytes;
-}
-
 namespace {
 
 GemmArgs f32_args(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t R, int64_t Cc,

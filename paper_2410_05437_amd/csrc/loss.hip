@@ -749,7 +749,7 @@ hipError_t launch_loss_prepare(const float* dloss, const int64_t* labels, const 
     return hipGetLastError();
 }
 
-// N < 2^21 tokens: at most 32768 workgroups of 64 rows in y
+// N < 2^21 tokens, K <= 2^21 features: at most 32768 workgroups of 64 rows in y
 static_assert((1 << 21) / 64 <= 65535, "launch limit");
 
 hipError_t launch_loss_grad(const Logits& S, int N, int c0, int cols, float inv_t, const float* lse,
@@ -778,17 +778,13 @@ hipError_t launch_loss_fix(const LossTargets& t, const float* picked, int64_t ld
 hipError_t launch_transpose_live(const void* X, int64_t ldx_, const float* r, int N, int K, void* dst, int64_t ldd,
                                  int64_t ldx, int terms, bool f32, const LiveTokens* live, hipStream_t stream) {
     const LiveTokens l = live ? *live : LiveTokens{};
-    // at most 65535 workgroups in y
-    for (int k0 = 0; k0 < K; k0 += 65535 * 64) {
-        const int k = K - k0 < 65535 * 64 ? K - k0 : 65535 * 64;
-        const dim3 grid((N + 63) / 64, (k + 63) / 64), block(256);
-        if (f32)
-            hipLaunchKernelGGL(transpose_live_kernel<float>, grid, block, 0, stream, (const float*)X + k0, ldx_, r, N,
-                               k, (float*)dst + (int64_t)k0 * ldd, ldd, ldx, terms, l);
-        else
-            hipLaunchKernelGGL(transpose_live_kernel<uint16_t>, grid, block, 0, stream, (const uint16_t*)X + k0, ldx_,
-                               r, N, k, (uint16_t*)dst + (int64_t)k0 * ldd, ldd, ldx, terms, l);
-    }
+    const dim3 grid((N + 63) / 64, (K + 63) / 64), block(256);
+    if (f32)
+        hipLaunchKernelGGL(transpose_live_kernel<float>, grid, block, 0, stream, (const float*)X, ldx_, r, N, K,
+                           (float*)dst, ldd, ldx, terms, l);
+    else
+        hipLaunchKernelGGL(transpose_live_kernel<uint16_t>, grid, block, 0, stream, (const uint16_t*)X, ldx_, r, N, K,
+                           (uint16_t*)dst, ldd, ldx, terms, l);
     return hipGetLastError();
 }
 
