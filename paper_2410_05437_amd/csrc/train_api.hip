@@ -42,10 +42,9 @@ constexpr int64_t kLogits = (int64_t)1 << 25, kGrads = (int64_t)1 << 26;
 // Where the epilogues cannot take a call's leading dimensions: narrow pieces, which fit
 // any layout.
 constexpr int64_t kNarrow = 256;
-// Tokens up to which a bfloat16 entry of G is kept as the sum of two: the entries of a
-// few tokens carry their roundings alone (65 tokens of 8 teacher's entries: dX and dW
-// 2.4e-3 off, 1.7e-3 with two, the rounding of the results), and the products of so few
-// are bound by reading W.
+// Tokens up to which a bfloat16 entry of G is kept as the sum of two: the products of so
+// few are bound by reading W, so a second term costs little (65 tokens of 8 teacher's
+// entries: dX and dW 2.4e-3 off, 1.7e-3 with two, the rounding of the results).
 constexpr int64_t kTwoTerms = 128;
 // Depth ranges of the logits' and dX's products whose sums the next pass adds, and the
 // floats of them.
