@@ -179,8 +179,10 @@ void gemm_tn_f32_mfma_kernel(const float* __restrict__ A, int64_t lda, const flo
     }
 }
 
-// x as the sum of three bfloat16: each rounds what the ones before it leave, whose
-// differences float32 holds exactly.  8 values to three 16-byte chunks.
+// x as the sum of three bfloat16 (Henry, Tang and Heinecke, "Leveraging the bfloat16
+// artificial intelligence datatype for higher-precision computations", ARITH 2019): each
+// rounds what the ones before it leave, whose differences float32 holds exactly.  8 values
+// to three 16-byte chunks.
 __device__ __forceinline__ void split3(f32x4_t lo, f32x4_t hi, u32x4_t (&t)[3]) {
     float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
